@@ -41,8 +41,8 @@
  *   - Every argument is checked before the first launch: a call that returns
  *     an error other than MUON_ERR_DEVICE changed nothing.  Values inside the
  *     tensors are never checked; NaN and Inf propagate.  The calls that
- *     launch work (muon_step, ns_orthogonalize_batched, muon_adamw_step) also
- *     ask the runtime about every buffer: it must start in device memory of
+ *     launch work (muon_step, ns_orthogonalize_batched, muon_adamw_step, the
+ *     attention block's) also ask the runtime about every buffer: it must start in device memory of
  *     the handle's device (or managed memory), and if it reaches beyond the
  *     allocation that holds its start, its last byte must be such memory too
  *     (allocations mapped back to back); otherwise MUON_ERR_INVALID_ARGUMENT.  muon_validate_step does not query the
@@ -294,6 +294,142 @@ typedef struct {
 muon_status_t muon_adamw_step(muon_handle_t h, const muon_adamw_param_t* params, int64_t n,
                               const muon_adamw_hparams_t* hp, void* stream);
 
+/*
+ * The attention block of a training step, for models whose query and key
+ * weights are clipped by their attention logits (QK-clip, the post-processing
+ * stage that Sec. 6.2 names): rotary positions, attention that also finds each
+ * head's largest logit, its backward pass, and the clip itself.
+ *
+ * These calls use nothing of the handle but its device, its error message and
+ * its timing: no workspace, table or event.  Scratch memory is the caller's
+ * (muon_attention_scratch), so that calls may be captured into graphs and
+ * issued on several streams at once as long as each has scratch of its own.
+ *
+ * A muon_heads_t is an array [batch][tokens][heads][head_dim] whose head_dim
+ * elements are contiguous; strides in elements.  data and strides must be
+ * multiples of 16 bytes (strides of dimensions of size 1 are ignored).
+ * Strides of an input may be 0 (a broadcast input); an output's elements must
+ * be distinct and must not meet any other buffer of the call.
+ */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} muon_heads_t;
+
+/*
+ * For query i of a sequence of Lq queries and Lk keys, and every query head h
+ * (keys and values of head h / (q_heads / kv_heads)):
+ *   key j is visible  iff  0 <= j < Lk, and with causal also j <= i + Lk - Lq,
+ *                          and with window > 0 also i + Lk - Lq - j < window
+ *   s_j   = scale * q_i . k_j          p_j = exp(s_j - lse_i)
+ *   lse_i = ln sum_j exp(s_j)          out_i = sum_j p_j v_j
+ * Where no key is visible, out_i = 0 and lse_i = -inf, and the gradients of
+ * that row are 0.
+ *
+ * Sequences.  Dense: `batch` sequences of q_tokens and k_tokens; q_lengths and
+ * k_lengths (device, int32, [batch], both or neither) cut them, and rows
+ * behind a length get out = 0, lse = -inf and zero gradients, whatever their
+ * inputs hold.  Packed: batch = 1, and q_offsets and k_offsets (device, int32,
+ * [sequences + 1], not decreasing, both or neither) cut the token axes into
+ * sequences; rows outside every sequence are left as they are.  Lengths and
+ * offsets beyond the axes are cut to them.
+ *
+ * Inputs that are not finite propagate; one that only some queries of a
+ * sequence may see can also reach the others (0 * inf).
+ */
+typedef struct {
+  int32_t dtype;           /* muon_dtype_t of q, k, v, out and gradients */
+  int32_t head_dim;        /* multiple of 8 (bf16) or 4 (fp32), 128 at most */
+  int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
+  int32_t causal;          /* 0 or 1 */
+  float scale;             /* finite, > 0 */
+  int64_t batch, q_tokens, k_tokens;
+  int64_t sequences;       /* of a packed request, else 0 */
+  int64_t window;          /* 0: none; otherwise needs causal */
+  const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
+  muon_heads_t q, k, v;
+  muon_heads_t out;
+  muon_heads_t residual;   /* bf16, or data = NULL: what the rounding took from
+                              out, rounded too.  The forward pass writes it,
+                              the backward pass adds it to out, whose rounding
+                              otherwise is the largest error of dq and dk */
+  float* lse;              /* [batch][q_heads][q_tokens], contiguous */
+  float* max_logits;       /* forward, [q_heads] or NULL: raised to the head's
+                              largest visible s_j (NaN is passed over) */
+  void* scratch;           /* muon_attention_scratch bytes, 256-byte aligned */
+  size_t scratch_bytes;
+} muon_attention_t;
+
+typedef struct {
+  muon_heads_t dout;       /* in: gradient of out */
+  muon_heads_t dq, dk, dv; /* out */
+} muon_attention_grad_t;
+
+/* Scratch bytes of a forward (backward = 0) or backward (1) pass: host only,
+ * from the sizes alone (no pointer is looked at).  0 is possible. */
+muon_status_t muon_attention_scratch(const muon_attention_t* a, int backward, size_t* bytes);
+/* Host-only checks of a forward (g NULL) or backward request: the status that
+ * the launching call would return before it asks the runtime about buffers;
+ * the reason goes into msg (may be NULL). */
+muon_status_t muon_validate_attention(const muon_attention_t* a, const muon_attention_grad_t* g, char* msg,
+                                      size_t msg_len);
+/* Writes out, lse, residual (if given) and max_logits (if given). */
+muon_status_t muon_attention_forward(muon_handle_t h, const muon_attention_t* a, void* stream);
+/* Writes dq, dk and dv from q, k, v, out, residual, lse and dout; the
+ * probabilities are recomputed.  Key and value gradients are summed over the
+ * query heads that share them.  Deterministic: no floating-point atomics. */
+muon_status_t muon_attention_backward(muon_handle_t h, const muon_attention_t* a, const muon_attention_grad_t* g,
+                                      void* stream);
+
+/* Rotary positions.  With p the position of a token and pairs (a, b) =
+ * (x_i, x_{i + r/2}) (layout 0) or (x_2i, x_2i+1) (layout 1), i < r/2, r =
+ * rotary_dim:  a' = scale (a cos t - b sin t),  b' = scale (a sin t + b cos t),
+ * t = p * freqs[i] (-p * freqs[i] with inverse, the gradient's form); the other
+ * elements of the head are copied.  Angles are formed and reduced in 64 bits,
+ * so far positions keep their accuracy. */
+typedef struct {
+  muon_heads_t x, y;       /* y may be x itself; otherwise they do not meet */
+  int64_t heads;
+} muon_rotary_tensor_t;
+typedef struct {
+  int32_t dtype;           /* muon_dtype_t of all tensors */
+  int32_t head_dim;        /* 1 .. 1024 */
+  int32_t rotary_dim;      /* even, 2 .. head_dim */
+  int32_t layout;          /* 0: halves, 1: neighbours */
+  int32_t inverse;         /* 0 or 1 */
+  float scale;             /* finite */
+  int64_t batch, tokens;
+  const void* positions;   /* device, or NULL: 0, 1, .. along the tokens */
+  int64_t position_batch_stride, position_token_stride;  /* elements */
+  int64_t first_position;  /* added to every position */
+  const double* freqs;     /* device, rotary_dim / 2, radians a position */
+  int32_t positions_int64; /* positions are int64 (else int32) */
+  int32_t n_tensors;       /* 1 .. 4 */
+} muon_rotary_t;
+/* Tensors may have any element alignment here (16-byte aligned ones with
+ * rotary_dim a multiple of 16 in bf16, of 8 in fp32, are faster). */
+muon_status_t muon_rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_tensor_t* tensors, void* stream);
+
+/* QK-clip of n pairs of weights.  wq is [q_heads * head_dim][cols], wk
+ * [kv_heads * head_dim][cols], row strides q_ld and k_ld (elements, 0 = cols).
+ * With M_h = max_logits[h], g_h = min(1, threshold / M_h) where M_h > threshold
+ * (1 otherwise and where M_h is not finite) and G = min g_h over the query
+ * heads that share a key head:
+ *   wk (its rows) *= sqrt(G)        wq (rows of h) *= g_h / sqrt(G)
+ * so that head h's logits scale by g_h.  Rows whose factor is 1 are not
+ * touched.  reset: then every max_logits entry becomes -inf, for the next
+ * step's attention to raise. */
+typedef struct {
+  void *wq, *wk;           /* in/out */
+  float* max_logits;       /* device, [q_heads] */
+  int64_t q_ld, k_ld, cols;
+  int32_t q_heads, kv_heads, head_dim;
+  int32_t dtype;           /* muon_dtype_t of wq and wk */
+  float threshold;         /* finite, > 0 */
+  int32_t reserved;        /* must be 0 */
+} muon_qk_clip_t;
+muon_status_t muon_qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n, int reset, void* stream);
+
 /* Host-only checks and planning (no device needed).  muon_validate_step
  * returns the status muon_step would return for these arguments before
  * launching anything and writes the reason into msg (may be NULL). */
@@ -325,7 +461,9 @@ muon_status_t muon_plan_step(const muon_param_t* params, int64_t n, const muon_h
  * gram_syrk, poly_syrk, update_gemm, update_apply_gemm,
  * apply_x0, adamw, ns_small (the whole step of a chunk whose short side is
  * at most 128, one launch in the count although column slices are 2 K + 2
- * kernels).  exec_flops of fp32 Newton-Schulz on the tile kernel counts its
+ * kernels), rotary, attention_forward, attention_backward, qk_clip (each call
+ * one launch in the count; the flops of attention are those of its products
+ * over the visible pairs of dense sequences).  exec_flops of fp32 Newton-Schulz on the tile kernel counts its
  * six bf16 products.  `reset` != 0 clears the counters after reading. */
 typedef struct {
   const char* name;

@@ -75,11 +75,54 @@ class MuonKernelStats(ctypes.Structure):
                 ("exec_flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class MuonHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class MuonAttention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("batch", ctypes.c_int64), ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
+                ("sequences", ctypes.c_int64), ("window", ctypes.c_int64),
+                ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
+                ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p),
+                ("q", MuonHeads), ("k", MuonHeads), ("v", MuonHeads), ("out", MuonHeads),
+                ("residual", MuonHeads), ("lse", ctypes.c_void_p), ("max_logits", ctypes.c_void_p),
+                ("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_size_t)]
+
+
+class MuonAttentionGrad(ctypes.Structure):
+    _fields_ = [("dout", MuonHeads), ("dq", MuonHeads), ("dk", MuonHeads), ("dv", MuonHeads)]
+
+
+class MuonRotaryTensor(ctypes.Structure):
+    _fields_ = [("x", MuonHeads), ("y", MuonHeads), ("heads", ctypes.c_int64)]
+
+
+class MuonRotary(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("inverse", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("positions", ctypes.c_void_p),
+                ("position_batch_stride", ctypes.c_int64), ("position_token_stride", ctypes.c_int64),
+                ("first_position", ctypes.c_int64), ("freqs", ctypes.c_void_p),
+                ("positions_int64", ctypes.c_int32), ("n_tensors", ctypes.c_int32)]
+
+
+class MuonQKClip(ctypes.Structure):
+    _fields_ = [("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p), ("max_logits", ctypes.c_void_p),
+                ("q_ld", ctypes.c_int64), ("k_ld", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("threshold", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 EXPORTS = ["muon_create", "muon_destroy", "muon_reserve", "muon_set_workspace_limit",
            "muon_workspace_bytes", "muon_step", "ns_orthogonalize_batched",
            "muon_validate_step", "muon_plan_step", "muon_status_string", "muon_last_error",
            "muon_abi_version", "muon_profile_enable", "muon_profile_read", "muon_adamw_step",
-           "muon_set_streams", "ns_orthogonalize_batched_noalloc", "muon_stream_copy"]
+           "muon_set_streams", "ns_orthogonalize_batched_noalloc", "muon_stream_copy",
+           "muon_attention_scratch", "muon_validate_attention", "muon_attention_forward",
+           "muon_attention_backward", "muon_rotary", "muon_qk_clip"]
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -122,6 +165,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.muon_status_string.restype = ctypes.c_char_p
     lib.muon_last_error.argtypes = [vp]
     lib.muon_last_error.restype = ctypes.c_char_p
+    # requests as packed bytes or ctypes structures
+    lib.muon_attention_scratch.argtypes = [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.muon_validate_attention.argtypes = [vp, vp, ctypes.c_char_p, ctypes.c_size_t]
+    lib.muon_attention_forward.argtypes = [vp, vp, vp]
+    lib.muon_attention_backward.argtypes = [vp, vp, vp, vp]
+    lib.muon_rotary.argtypes = [vp, vp, vp, vp]
+    lib.muon_qk_clip.argtypes = [vp, vp, i64, ctypes.c_int, vp]
+    for name in ("muon_attention_scratch", "muon_validate_attention", "muon_attention_forward",
+                 "muon_attention_backward", "muon_rotary", "muon_qk_clip"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("muon_create", "muon_destroy", "muon_reserve", "muon_set_workspace_limit",
                  "muon_step", "ns_orthogonalize_batched", "muon_validate_step", "muon_plan_step",
                  "muon_profile_enable", "muon_profile_read", "muon_adamw_step", "muon_set_streams",
@@ -317,6 +370,78 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+# Requests of the attention block as packed records (a test compares them with
+# the ctypes layouts): filling ctypes fields takes longer than a small call.
+_HEADS = "Pqqq"
+_ATTENTION_PACK = struct.Struct("@iiiiif5q4P" + 5 * _HEADS + "PPPN")
+_GRAD_PACK = struct.Struct("@" + 4 * _HEADS)
+_ROTARY_PACK = struct.Struct("@iiiiifqqPqqqPii")
+_ROTARY_TENSOR_PACK = struct.Struct("@" + 2 * _HEADS + "q")
+_CLIP_PACK = struct.Struct("@PPPqqqiiiifi")
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads(t):
+    """(pointer, batch stride, token stride, head stride) of [B, S, H, D] or [S, H, D]."""
+    st = t.stride()
+    if t.shape[-1] > 1 and st[-1] != 1:
+        raise ValueError("the elements of a head must be contiguous")
+    return (t.data_ptr(), st[0], st[1], st[2]) if len(st) == 4 else (t.data_ptr(), 0, st[0], st[1])
+
+
+class _Attention:
+    """One attention request: checks that need the tensors' shapes, then the
+    library's packed record."""
+
+    def __init__(self, q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens):
+        import torch
+        packed = q_offsets is not None or k_offsets is not None
+        nd = 3 if packed else 4
+        if q.dim() != nd or k.dim() != nd or v.shape != k.shape:
+            raise ValueError("attention takes q [B, Sq, Hq, D] and k, v [B, Sk, Hkv, D], or without B and with "
+                             "q_offsets and k_offsets")
+        if q.shape[-1] != k.shape[-1] or (nd == 4 and q.shape[0] != k.shape[0]):
+            raise ValueError("q and k differ in batch or head size")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise TypeError("q, k and v must share one dtype")
+        self.code = _dtype_code(q)
+        batch = 1 if packed else q.shape[0]
+        self.lists = (q_offsets, k_offsets, q_lens, k_lens)
+        seqs = 0
+        for i, t in enumerate(self.lists):
+            if t is None:
+                continue
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+                raise TypeError("offsets and lengths must be contiguous 1-D int32 tensors")
+            if i < 2:
+                if t.numel() < 1 or (seqs and t.numel() - 1 != seqs):
+                    raise ValueError("q_offsets and k_offsets must have equal length, >= 1")
+                seqs = t.numel() - 1
+            elif t.numel() != batch:
+                raise ValueError(f"lengths must have {batch} entries")
+        sq, hq, d = q.shape[-3:]
+        sk, hkv = k.shape[-3], k.shape[-2]
+        self.lse_shape = (hq, sq) if packed else (batch, hq, sq)
+        self.q_shape, self.k_shape = q.shape, k.shape
+        self.head = (self.code, d, hq, hkv, int(bool(causal)), float(d) ** -0.5 if scale is None else float(scale),
+                     batch, sq, sk, seqs, int(window),
+                     *(0 if t is None else t.data_ptr() for t in self.lists), *_heads(q), *_heads(k), *_heads(v))
+
+    def record(self, out, residual, lse, max_logits, scratch, scratch_bytes):
+        return _ATTENTION_PACK.pack(*self.head, *_heads(out), *(_NO_HEADS if residual is None else _heads(residual)),
+                                    lse.data_ptr(), 0 if max_logits is None else max_logits.data_ptr(), scratch,
+                                    scratch_bytes)
+
+    def sizes(self):
+        """The record with no outputs yet, for muon_attention_scratch."""
+        return _ATTENTION_PACK.pack(*self.head, *_NO_HEADS, *_NO_HEADS, 0, 0, 0, 0)
+
+
+def _expect(t, shape, dtype, what):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+
+
 class Muon:
     """A library handle on one device; owns the workspace."""
 
@@ -459,6 +584,181 @@ class Muon:
             ctypes.cast(coeff, ctypes.POINTER(ctypes.c_float)) if coeff else None,
             float(eps), NS_F32 if ns_precision == "f32" else NS_BF16,
             ctypes.c_void_p(_stream_ptr(stream))))
+
+    # ---- the attention block of a training step ---------------------------------
+
+    def _on(self, stream):
+        """(stream pointer, context): outputs and scratch are allocated on the
+        stream that the call runs on."""
+        import contextlib
+        import torch
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream, contextlib.nullcontext()
+        return stream.cuda_stream, torch.cuda.stream(stream)
+
+    def _scratch(self, record, backward):
+        """(keepalive, pointer, bytes) of the scratch memory a request needs."""
+        import torch
+        n = ctypes.c_size_t()
+        st = self.lib.muon_attention_scratch(record, backward, ctypes.byref(n))
+        if st != MUON_OK:  # the message comes with the host-only checks
+            msg = ctypes.create_string_buffer(256)
+            self.lib.muon_validate_attention(record, None, msg, 256)
+            raise MuonError(st, msg.value.decode())
+        if n.value == 0:
+            return None, 0, 0
+        t = torch.empty(n.value + 256, dtype=torch.uint8, device=torch.device("cuda", self.device))
+        return t, (t.data_ptr() + 255) & ~255, n.value
+
+    def attention(self, q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None,
+                  k_lens=None, max_logits=None, out=None, residual=None, stream=None):
+        """(out, lse) of softmax attention (muon_attention_forward).
+
+        q is [B, Sq, Hq, D], k and v [B, Sk, Hkv, D] (any strides with
+        contiguous heads, 16-byte aligned; slices of a fused tensor are fine),
+        Hq a multiple of Hkv; with q_offsets and k_offsets (int32, [n + 1])
+        the token axes hold n packed sequences and there is no batch axis;
+        q_lens and k_lens (int32, [B]) cut a padded batch.  `scale` defaults to
+        D ** -0.5.  `causal` aligns the last query with the last key; `window`
+        keeps the last `window` keys of each query.  max_logits (fp32, [Hq]) is
+        raised to each head's largest logit.  residual (bf16, like out)
+        receives what the rounding took from out, for attention_backward.
+        lse is fp32, [B, Hq, Sq] ([Hq, Sq] packed)."""
+        import torch
+        a = _Attention(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+        _check_device([t for t in (q, k, v, max_logits, out, residual, *a.lists) if t is not None], self.device)
+        if max_logits is not None:
+            _expect(max_logits, (q.shape[-2],), torch.float32, "max_logits")
+            if not max_logits.is_contiguous():
+                raise ValueError("max_logits must be contiguous")
+        for t, what in ((out, "out"), (residual, "residual")):
+            if t is not None:
+                _expect(t, q.shape, q.dtype, what)
+        ptr, ctx = self._on(stream)
+        with ctx:
+            keep, at, n = self._scratch(a.sizes(), 0)
+            if out is None:  # rows outside packed sequences are not written
+                out = (torch.empty if q_offsets is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+            lse = (torch.empty(a.lse_shape, dtype=torch.float32, device=q.device) if q_offsets is None else
+                   torch.full(a.lse_shape, -float("inf"), dtype=torch.float32, device=q.device))
+            self._check(self.lib.muon_attention_forward(self.h, a.record(out, residual, lse, max_logits, at, n), ptr))
+            del keep
+        return out, lse
+
+    def attention_backward(self, dout, q, k, v, out, lse, residual=None, scale=None, causal=False, window=0,
+                           q_offsets=None, k_offsets=None, q_lens=None, k_lens=None, dq=None, dk=None, dv=None,
+                           stream=None):
+        """(dq, dk, dv) of attention (muon_attention_backward) from its inputs,
+        its results and the gradient of out; the other arguments as the
+        forward pass had them.  dq, dk, dv may be given (slices of one tensor
+        are fine)."""
+        import torch
+        a = _Attention(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
+        _check_device([t for t in (dout, q, k, v, out, lse, residual, dq, dk, dv, *a.lists) if t is not None],
+                      self.device)
+        for t, like, what in ((dout, q, "dout"), (out, q, "out"), (residual, q, "residual"), (dq, q, "dq"),
+                              (dk, k, "dk"), (dv, v, "dv")):
+            if t is not None:
+                _expect(t, like.shape, q.dtype, what)
+        _expect(lse, a.lse_shape, torch.float32, "lse")
+        if not lse.is_contiguous():
+            raise ValueError("lse must be contiguous")
+        ptr, ctx = self._on(stream)
+        with ctx:
+            keep, at, n = self._scratch(a.sizes(), 1)
+            new = torch.empty if q_offsets is None else torch.zeros
+            dq = new(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+            dk = new(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
+            dv = new(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+            grad = _GRAD_PACK.pack(*_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv))
+            self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n), grad, ptr))
+            del keep
+        return dq, dk, dv
+
+    def rotary(self, xs, freqs, positions=None, first=0, layout="half", scale=1.0, inverse=False, outs=None,
+               stream=None):
+        """Rotary positions (muon_rotary) of one tensor [B, S, H, D] (or
+        [S, H, D]) or of up to 4 that differ in H only, in one launch; returns
+        the result(s).  freqs: fp64, [r / 2], radians a position; the first r
+        elements of each head turn.  positions: int32 or int64, [B, S] ([S]),
+        any strides, or None for 0 .. S - 1; `first` is added.  layout: "half"
+        (x_i with x_{i + r/2}) or "interleaved" (x_2i with x_2i+1).  inverse
+        turns backwards: the gradient's form.  outs: results' tensors; the
+        inputs themselves for in place."""
+        import torch
+        one = torch.is_tensor(xs)
+        xs = [xs] if one else list(xs)
+        if not 1 <= len(xs) <= 4:
+            raise ValueError("rotary takes 1 to 4 tensors")
+        if layout not in ("half", "interleaved"):
+            raise ValueError(f"layout must be 'half' or 'interleaved', got {layout!r}")
+        x = xs[0]
+        if x.dim() not in (3, 4):
+            raise ValueError("rotary takes [B, S, H, D] or [S, H, D]")
+        lead, d = tuple(x.shape[:-2]), x.shape[-1]
+        for t in xs[1:]:
+            if tuple(t.shape[:-2]) != lead or t.shape[-1] != d or t.dim() != x.dim():
+                raise ValueError("the tensors of a call may differ in their number of heads only")
+            if t.dtype != x.dtype:
+                raise TypeError("the tensors of a call must share one dtype")
+        if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+            raise TypeError("freqs must be a contiguous 1-D float64 tensor")
+        if positions is not None:
+            if positions.dtype not in (torch.int32, torch.int64):
+                raise TypeError("positions must be int32 or int64")
+            if tuple(positions.shape) != lead:
+                raise ValueError(f"positions must have shape {lead}")
+        if outs is not None:
+            outs = [outs] if torch.is_tensor(outs) else list(outs)
+            if len(outs) != len(xs):
+                raise ValueError("outs must have one tensor for each input")
+            for t, y in zip(xs, outs):
+                _expect(y, t.shape, t.dtype, "out")
+        _check_device([*xs, freqs, *([] if positions is None else [positions]), *(outs or [])], self.device)
+        ptr, ctx = self._on(stream)
+        with ctx:
+            if outs is None:
+                outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
+            batch, tokens = lead if len(lead) == 2 else (1, lead[0])
+            pst = (0, 0) if positions is None else (positions.stride() if len(lead) == 2 else (0, positions.stride(0)))
+            rec = _ROTARY_PACK.pack(_dtype_code(x), d, 2 * freqs.numel(), int(layout == "interleaved"),
+                                    int(bool(inverse)), float(scale), batch, tokens,
+                                    0 if positions is None else positions.data_ptr(), *pst, int(first),
+                                    freqs.data_ptr(), int(positions is not None and positions.dtype == torch.int64),
+                                    len(xs))
+            ts = b"".join(_ROTARY_TENSOR_PACK.pack(*_heads(t), *_heads(y), t.shape[-2]) for t, y in zip(xs, outs))
+            self._check(self.lib.muon_rotary(self.h, rec, ts, ptr))
+        return outs[0] if one else outs
+
+    def qk_clip(self, wqs, wks, max_logits, threshold, reset=False, stream=None):
+        """In place: scales the rows of query weights wqs[i] [Hq * hd, cols] and
+        key weights wks[i] [Hkv * hd, cols] so that every head whose largest
+        logit max_logits[i] (fp32, [Hq]) exceeds `threshold` comes down to it
+        (muon_qk_clip).  reset: the logits become -inf afterwards."""
+        import torch
+        n = len(wqs)
+        if not (len(wks) == len(max_logits) == n):
+            raise ValueError("query weights, key weights and logits must have equal length")
+        _check_device([*wqs, *wks, *max_logits], self.device)
+        recs = []
+        for i, (q, k, m) in enumerate(zip(wqs, wks, max_logits)):
+            if q.dim() != 2 or k.dim() != 2 or q.shape[1] != k.shape[1] or q.dtype != k.dtype:
+                raise ValueError(f"entry {i}: weights must be matrices of one dtype and one number of columns")
+            if m.dtype != torch.float32 or m.dim() != 1 or not m.is_contiguous() or m.numel() < 1:
+                raise TypeError(f"entry {i}: logits must be a contiguous 1-D float32 tensor")
+            hq, (rows, cols) = m.numel(), q.shape
+            hd = rows // hq
+            if rows % hq or hd == 0 or k.shape[0] % hd or k.shape[0] == 0:
+                raise ValueError(f"entry {i}: {rows} query rows and {k.shape[0]} key rows are not whole heads of {hq}")
+            for t in (q, k):
+                if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
+                    raise ValueError(f"entry {i}: rows must be contiguous and distinct")
+            recs.append(_CLIP_PACK.pack(q.data_ptr(), k.data_ptr(), m.data_ptr(), q.stride(0) if rows > 1 else cols,
+                                        k.stride(0) if k.shape[0] > 1 else cols, cols, hq, k.shape[0] // hd, hd,
+                                        _dtype_code(q), float(threshold), 0))
+        ptr, ctx = self._on(stream)
+        with ctx:
+            self._check(self.lib.muon_qk_clip(self.h, b"".join(recs), n, int(bool(reset)), ptr))
 
 
 def validate_step(entries: Sequence[MuonParam], hp: MuonHParams):

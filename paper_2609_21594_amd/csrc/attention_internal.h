@@ -1,0 +1,99 @@
+// Internal interface between the attention entry points (attention_api.hip)
+// and their gfx950 kernels (attention_kernels.hip).  Not installed.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "muon_internal.h"
+
+namespace muon {
+
+// A [batch, tokens, heads, head_dim] array: strides in bytes, head_dim
+// contiguous.
+struct Heads {
+  char* p;
+  int64_t batch, token, head;
+};
+
+// Sequences of a call.  Dense: `batch` sequences of q_tokens and k_tokens,
+// each cut to q_len[b] / k_len[b] where given.  Packed (q_off given): n_seq
+// sequences one behind the other on one token axis, sequence s being
+// [off[s], off[s + 1]).  The device values are clamped to the token axes
+// before use, so that no value reaches an address outside them.
+struct Seqs {
+  int64_t batch;
+  int32_t q_tokens, k_tokens, n_seq;
+  const int32_t *q_off, *k_off, *q_len, *k_len;
+};
+
+struct AttnArgs {
+  Heads q, k, v, out, res, dout, dq, dk, dv;
+  Seqs seqs;
+  int32_t q_heads, kv_heads, group, dim;
+  int32_t causal, window;
+  float scale, scale2;       // scale2 = scale * log2(e)
+  float* lse;                // [batch][q_heads][q_tokens], natural logarithm
+  float* max_logits;         // [q_heads] or null
+  // forward, split over the keys: per split and row the unnormalised output
+  // (fp32) and its maximum and sum
+  int32_t splits;
+  float* part_o;             // [splits][rows][dim]
+  float2* part_ml;           // [splits][rows]
+  // backward: per row log2(sum exp) (+inf where nothing is visible) and
+  // dout . out
+  float *lse2, *delta;
+  // backward, heads of a group in workgroups of their own: fp32 gradients per
+  // query head, [batch * k_tokens][q_heads][dim] (packed: [k_tokens][..])
+  int32_t kv_split;
+  float *part_dk, *part_dv;
+};
+
+hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
+hipError_t run_attention_backward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
+// Over how many parts of the key axis the forward pass of this request is
+// spread (1: none), and whether its backward pass gives every query head
+// workgroups of its own for the key and value gradients.
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype, bool causal, int window);
+bool backward_splits_heads(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype);
+
+constexpr int kRotaryMax = 4;
+struct RotaryTensor {
+  Heads x, y;
+  int32_t heads;
+  int32_t vec;               // 16-byte accesses
+};
+struct RotaryArgs {
+  RotaryTensor t[kRotaryMax];
+  int32_t n;
+  int64_t batch, tokens;
+  const void* positions;     // null: 0, 1, .. along the tokens
+  int32_t positions64;       // int64 (else int32)
+  int64_t pos_batch, pos_token;  // strides in elements
+  int64_t first;             // added to every position
+  const double* freqs;       // dim_rot / 2, radians a position
+  int32_t dim, rot, interleaved;
+  float scale, sign;
+};
+hipError_t run_rotary(const RotaryArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
+
+constexpr int kClipMax = 32;
+struct ClipEntry {
+  char *wq, *wk;
+  int64_t ldq, ldk;          // bytes
+  float* logits;
+  int32_t q_heads, kv_heads, dim, cols;
+  int32_t vec;
+  float threshold;
+};
+struct ClipArgs {
+  ClipEntry e[kClipMax];
+  int32_t first[kClipMax + 1];  // first workgroup of each entry
+  int32_t n;
+};
+hipError_t run_qk_clip(const ClipArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
+hipError_t run_reset_logits(const ClipArgs& a, hipStream_t st);
+// Rows of a weight one workgroup of the clip takes.
+constexpr int kClipRows = 8;
+
+}  // namespace muon

@@ -1,0 +1,1118 @@
+// gfx950 kernels of the attention block: rotary positions, attention forward
+// and backward, the clip of query and key weights by their heads' logits.
+//
+// Attention works on 32-row MFMA blocks whose accumulator layout makes the
+// next product's operand: with S^T = K Q^T (A = K rows from LDS, B = Q rows in
+// registers) a lane holds, for the one query lane % 32, the 4 consecutive keys
+// 8g + 4 (lane / 32) + i of every group g of 8.  The contraction over keys of
+// the next product may take the keys in any order as long as both operands
+// agree, so these registers, rounded and packed, are its B operand as they
+// lie, and the A operand (V^T, K^T) takes the same keys through transposing
+// LDS reads.  Row statistics of a softmax are then per lane (plus one exchange
+// between the halves of the wave).  The key/value gradient swaps the roles:
+// S = Q K^T with keys in the lanes, and dV^T = dO^T P, dK^T = Q^T dS.
+//
+// LDS tiles keep rows of DP elements; the 16-byte chunk c of row r lies at
+// chunk c ^ key(r), so that both the 16-byte reads of 32 rows at one chunk and
+// the transposing reads of 4 rows at 4 chunks spread over the banks.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_internal.h"
+#include "gfx950_util.h"
+
+namespace muon {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_huge_valf();
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x of the lane in the other half of the wave, combined.
+__device__ __forceinline__ uint2 swap32(uint32_t a, uint32_t b) {
+  const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return make_uint2(v[0], v[1]);
+}
+__device__ __forceinline__ float max32(float x) {
+  const uint2 v = swap32(__float_as_uint(x), __float_as_uint(x));
+  return fmaxf(__uint_as_float(v.x), __uint_as_float(v.y));
+}
+__device__ __forceinline__ float sum32(float x) {
+  const uint2 v = swap32(__float_as_uint(x), __float_as_uint(x));
+  return __uint_as_float(v.x) + __uint_as_float(v.y);
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return max32(x);
+}
+// The order of finite floats and infinities is that of their bits as signed
+// integers where positive, reversed as unsigned ones where negative; x is no
+// NaN.  Maxima do not depend on the order of the updates.
+__device__ __forceinline__ void atomic_max_f32(float* p, float x) {
+  x += 0.f;  // no negative zero
+  if (x >= 0.f) atomicMax(reinterpret_cast<int*>(p), __float_as_int(x));
+  else atomicMin(reinterpret_cast<unsigned*>(p), __float_as_uint(x));
+}
+
+template <typename T, int DP>
+struct Lay {
+  static constexpr int ES = sizeof(T), EPC = 16 / ES, CH = DP / EPC, RB = DP * ES;
+  static constexpr int STEPS = CH / 2;   // MFMA steps over the head: 2 chunks each, one per half of the wave
+  static constexpr int DB = DP / 32;     // 32-row blocks of the head
+  __device__ __forceinline__ static int key(int r) {
+    if constexpr (CH == 8) return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3);
+    else return ((r & 3) << 2) | ((r >> 2) & 3);
+  }
+  __device__ __forceinline__ static int at(int r, int c) { return r * RB + ((c ^ key(r)) << 4); }
+};
+
+__device__ __forceinline__ u32x4_t lds16(const char* p) { return *reinterpret_cast<const u32x4_t*>(p); }
+
+// Stages ROWS rows of `dch` chunks (base: row 0, stride in bytes) into LDS by
+// direct loads of the whole workgroup of 256.  Rows from `left` on repeat the
+// last one and chunks from dch on the last one: what they hold is finite where
+// the operand is, and meets zeros or is never read.
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ void stage_rows(const char* base, uint32_t stride, int left, int dch, uint32_t lds) {
+  using L = Lay<T, DP>;
+  static_assert(ROWS * L::CH % 256 == 0, "whole loads");
+  const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < ROWS * L::CH / 256; ++i) {
+    const int p = i * 256 + threadIdx.x, r = p / L::CH;
+    const int c = min((p % L::CH) ^ L::key(r), dch - 1);
+    load_lds16(base, static_cast<uint32_t>(min(r, left - 1)) * stride + c * 16, lds + (i * 256 + wave * 64) * 16);
+  }
+}
+
+// The lane's row of an operand kept in registers: chunks 2 s + half, zeros
+// beyond the head.
+template <typename T, int DP>
+__device__ __forceinline__ void load_operand(const char* row, int dch, int half, u32x4_t* f) {
+  using L = Lay<T, DP>;
+#pragma unroll
+  for (int s = 0; s < L::STEPS; ++s) {
+    const int c = 2 * s + half;
+    f[s] = c < dch ? *reinterpret_cast<const u32x4_t*>(row + c * 16) : u32x4_t{0, 0, 0, 0};
+  }
+}
+
+// A operand of the contraction over the head: rows r0 + lane % 32 of a tile.
+template <typename T, int DP>
+__device__ __forceinline__ u32x4_t frag_rows(const char* tile, int r0, int s, int lane) {
+  return lds16(tile + Lay<T, DP>::at(r0 + (lane & 31), 2 * s + (lane >> 5)));
+}
+// Steps of a contraction over 32 tile rows: 16 rows each (bf16), 8 (fp32).
+template <typename T> constexpr int kRowSteps = sizeof(T) == 2 ? 2 : 4;
+// A operand of the contraction over tile rows: elements 32 db + lane % 32 of
+// the rows that step `st` of accumulator block rows r0 .. r0 + 31 holds.
+template <typename T, int DP>
+__device__ __forceinline__ u32x4_t frag_cols(const char* tile, int r0, int st, int db, int lane) {
+  using L = Lay<T, DP>;
+  if constexpr (sizeof(T) == 2) {
+    const int G = lane >> 4, q = lane & 15;
+    const int r = r0 + 16 * st + 4 * (G >> 1) + (q >> 2), c = 4 * db + 2 * (G & 1) + ((q & 3) >> 1);
+    const uint2 lo = tr_read_b64(tile + L::at(r, c) + (q & 1) * 8), hi = tr_read_b64(tile + L::at(r + 8, c) + (q & 1) * 8);
+    return u32x4_t{lo.x, lo.y, hi.x, hi.y};
+  } else {
+    u32x4_t f;
+    const int d = 32 * db + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      f[i] = *reinterpret_cast<const uint32_t*>(tile + L::at(r0 + 8 * st + 4 * (lane >> 5) + i, d >> 2) + (d & 3) * 4);
+    return f;
+  }
+}
+// The B operand of that step: accumulator registers, rounded for bf16.
+template <typename T>
+__device__ __forceinline__ u32x4_t frag_acc(const f32x16_t& s, int st) {
+  u32x4_t f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) f[i] = pack_bf16x2(s[8 * st + 2 * i], s[8 * st + 2 * i + 1]);
+    else f[i] = __float_as_uint(s[4 * st + i]);
+  }
+  return f;
+}
+
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// Writes the lane's row (a transposed accumulator: element 32 db + 8 g +
+// 4 half + i in register 4 g + i of block db), times `f`.  RES: to `res` goes
+// what the rounding took.  All lanes of the wave call it; `on`: this lane
+// writes.
+template <typename T, int DB>
+__device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row, char* res, int dch, int half, bool on) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        uint32_t w[4], e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {  // k / 2: group 2 p + k / 2, pairs of elements
+          const float x = o[db][8 * p + 2 * k] * f, y = o[db][8 * p + 2 * k + 1] * f;
+          w[k] = pack_bf16x2(x, y);
+          e[k] = res ? pack_bf16x2(x - __uint_as_float(w[k] << 16), y - __uint_as_float(w[k] & 0xffff0000u)) : 0u;
+        }
+        // halves exchange so that each lane holds 8 consecutive elements
+        const uint2 a = swap32(w[0], w[2]), b = swap32(w[1], w[3]);
+        const int c = 4 * db + 2 * p + half;
+        if (on && c < dch) *reinterpret_cast<u32x4_t*>(row + c * 16) = u32x4_t{a.x, b.x, a.y, b.y};
+        if (res) {
+          const uint2 u = swap32(e[0], e[2]), v = swap32(e[1], e[3]);
+          if (on && c < dch) *reinterpret_cast<u32x4_t*>(res + c * 16) = u32x4_t{u.x, v.x, u.y, v.y};
+        }
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = 8 * db + 2 * g + half;
+        if (on && c < dch)
+          *reinterpret_cast<float4*>(row + c * 16) =
+              make_float4(o[db][4 * g] * f, o[db][4 * g + 1] * f, o[db][4 * g + 2] * f, o[db][4 * g + 3] * f);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Which work a workgroup has.
+// ---------------------------------------------------------------------------
+// Workgroup -> (batch, key head, head of the group, tile).  Workgroup b runs
+// on XCD b % 8: where the (batch, key head) units divide evenly, each XCD takes
+// whole units one after the other, so that the keys and values it works on fit
+// its L2; else tiles come first and units spread over all XCDs.  `reverse`
+// puts the last tiles (the longest of a causal pass) first.
+struct Item { int b, kvh, g, tile; };
+__device__ __forceinline__ Item item_of(int bid, const AttnArgs& a, int per_unit_heads, int tiles, bool reverse) {
+  const int units = static_cast<int>(a.seqs.batch) * a.kv_heads;
+  int unit, rest;
+  if (units % 8 == 0) {
+    const int j = bid >> 3, per = tiles * per_unit_heads;
+    unit = (bid & 7) * (units >> 3) + j / per;
+    rest = j % per;
+  } else {
+    unit = bid % units;
+    rest = bid / units;
+  }
+  Item it;
+  it.b = unit / a.kv_heads;
+  it.kvh = unit % a.kv_heads;
+  it.g = rest % per_unit_heads;
+  it.tile = rest / per_unit_heads;
+  if (reverse) it.tile = tiles - 1 - it.tile;
+  return it;
+}
+
+// A sequence: tokens q0 .. q0 + nq - 1 and k0 .. k0 + nk - 1 of batch b's
+// axes; the rows of it that are written are q_rows / k_rows (dense: the whole
+// axis, rows behind the length being zeros).  tile: of this sequence.
+struct Seq { int q0, nq, k0, nk, q_rows, k_rows, tile; bool ok; };
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// The sequence that holds tile `tile` of `bt` queries (keys where by_key).
+// Packed: the tiles of all sequences are numbered one after the other; each
+// wave counts them, 64 sequences at a time.
+__device__ __forceinline__ Seq find_seq(const Seqs& s, int b, int tile, int bt, bool by_key) {
+  Seq r;
+  r.ok = true;
+  r.tile = tile;
+  if (!s.q_off) {
+    r.q0 = r.k0 = 0;
+    r.nq = s.q_len ? clampi(s.q_len[b], 0, s.q_tokens) : s.q_tokens;
+    r.nk = s.k_len ? clampi(s.k_len[b], 0, s.k_tokens) : s.k_tokens;
+    r.q_rows = s.q_tokens;
+    r.k_rows = s.k_tokens;
+    return r;
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int s0 = 0; s0 < s.n_seq; s0 += 64) {
+    const int i = s0 + lane;
+    int q0 = 0, nq = 0, k0 = 0, nk = 0;
+    if (i < s.n_seq) {
+      q0 = clampi(s.q_off[i], 0, s.q_tokens);
+      nq = clampi(s.q_off[i + 1], q0, s.q_tokens) - q0;
+      k0 = clampi(s.k_off[i], 0, s.k_tokens);
+      nk = clampi(s.k_off[i + 1], k0, s.k_tokens) - k0;
+    }
+    const int n = ((by_key ? nk : nq) + bt - 1) / bt;
+    int upto = n;  // tiles of this lane's sequence and those before it
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    const unsigned long long hit = __ballot(before + upto > tile);
+    if (hit) {
+      const int l = __ffsll(hit) - 1;
+      r.tile = tile - before - __builtin_amdgcn_readlane(upto - n, l);
+      r.q0 = __builtin_amdgcn_readlane(q0, l);
+      r.nq = r.q_rows = __builtin_amdgcn_readlane(nq, l);
+      r.k0 = __builtin_amdgcn_readlane(k0, l);
+      r.nk = r.k_rows = __builtin_amdgcn_readlane(nk, l);
+      return r;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  r.q0 = r.nq = r.k0 = r.nk = r.q_rows = r.k_rows = 0;
+  r.ok = false;
+  return r;
+}
+
+__device__ __forceinline__ const char* at_row(const Heads& h, int b, int token, int head) {
+  return h.p + b * h.batch + token * h.token + head * h.head;
+}
+__device__ __forceinline__ char* at_row_w(const Heads& h, int b, int token, int head) {
+  return h.p + b * h.batch + token * h.token + head * h.head;
+}
+// Index of a row's log-sum-exp.
+__device__ __forceinline__ int64_t row_index(const AttnArgs& a, int b, int head, int token) {
+  return (static_cast<int64_t>(b) * a.q_heads + head) * a.seqs.q_tokens + token;
+}
+
+// Keys that queries lo .. hi (of one sequence) see: any of them [beg, end),
+// all of them [all_beg, all_end).
+struct KeyRange { int beg, end, all_beg, all_end; };
+__device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int lo, int hi) {
+  KeyRange r{0, s.nk, 0, s.nk};
+  if (hi < lo) return KeyRange{0, 0, 0, 0};
+  const int shift = s.nk - s.nq;
+  if (a.causal) {
+    r.end = clampi(hi + shift + 1, 0, s.nk);
+    r.all_end = clampi(lo + shift + 1, 0, s.nk);
+    if (a.window) {
+      r.beg = max(0, lo + shift - a.window + 1);
+      r.all_beg = max(0, hi + shift - a.window + 1);
+    }
+  }
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// Forward.  A workgroup of 4 waves holds 128 queries (32 a wave) and passes
+// over the keys in tiles of BN, double-buffered in LDS, keeping the running
+// maximum and sum.
+// ---------------------------------------------------------------------------
+template <typename T, int DP, int BN, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
+  using L = Lay<T, DP>;
+  constexpr int KB = BN / 32, STAGE = 2 * BN * L::RB;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int dch = a.dim / L::EPC;
+  int bid = blockIdx.x, split = 0;
+  if constexpr (SPLIT) {
+    const int items = gridDim.x / a.splits;
+    split = bid / items;
+    bid -= split * items;
+  }
+  const Item it = item_of(bid, a, pack ? 1 : a.group, tiles, a.causal);
+  const Seq s = find_seq(a.seqs, it.b, it.tile, 128, false);
+  if (!s.ok) return;
+  const int shift = s.nk - s.nq;
+
+  // the lane's row.  pack: the rows are all heads of the group, each with all queries
+  const int rows = pack ? s.q_rows * a.group : s.q_rows;
+  const int r0 = s.tile * 128 + wave * 32;
+  const bool in = r0 + (lane & 31) < rows;
+  int iq = min(r0 + (lane & 31), rows - 1), g = it.g;
+  if (pack) {
+    g = iq / s.q_rows;
+    iq -= g * s.q_rows;
+  }
+  const int head = it.kvh * a.group + g;
+  const bool live = in && iq < s.nq;
+  int jmax = s.nk - 1, jmin = 0;
+  if (a.causal) {
+    jmax = min(jmax, iq + shift);
+    if (a.window) jmin = max(0, iq + shift - a.window + 1);
+  }
+  u32x4_t qf[L::STEPS];
+  load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq, head), dch, half, qf);
+
+  // the keys of the workgroup and of the wave
+  const int last = min(s.q_rows, s.nq) - 1;
+  const KeyRange wg = pack ? keys_of(a, s, 0, last) : keys_of(a, s, s.tile * 128, min(s.tile * 128 + 127, last));
+  const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 31, last));
+  int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
+  if constexpr (SPLIT) {
+    const int per = (max(t1 - t0, 0) + a.splits - 1) / a.splits;
+    t0 += split * per;
+    t1 = min(t1, t0 + per);
+  }
+
+  const uint32_t lds0 = lds_offset(smem);
+  const uint32_t kst = static_cast<uint32_t>(a.k.token), vst = static_cast<uint32_t>(a.v.token);
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (t & 1) * STAGE;
+    const int j = t * BN;
+    stage_rows<T, DP, BN>(at_row(a.k, it.b, s.k0 + j, it.kvh), kst, s.nk - j, dch, at);
+    stage_rows<T, DP, BN>(at_row(a.v, it.b, s.k0 + j, it.kvh), vst, s.nk - j, dch, at + BN * L::RB);
+  };
+
+  f32x16_t o[L::DB];
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) o[db] = zero16();
+  float m = -kInf, l = 0.f, top = -kInf;
+  if (t0 < t1) issue(t0);
+  for (int t = t0; t < t1; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // tile t has landed, and every wave is done with tile t - 1
+    if (t + 1 < t1) issue(t + 1);
+    const int j0 = t * BN;
+    if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
+    const char* ks = smem + (t & 1) * STAGE;
+    const char* vs = ks + BN * L::RB;
+    f32x16_t p[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) p[kb] = zero16();
+#pragma unroll
+    for (int st = 0; st < L::STEPS; ++st)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) Mma<T>::run(frag_rows<T, DP>(ks, 32 * kb, st, lane), qf[st], p[kb]);
+    if (j0 + BN > wv.all_end || j0 < wv.all_beg) {
+      const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+          if (j < lo || j > hi) p[kb][r] = -kInf;
+        }
+    }
+    float mx = -kInf;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[kb][r]);
+    mx = max32(mx);
+    top = fmaxf(top, mx);
+    const float mn = fmaxf(m, mx * a.scale2);
+    const float mu = mn == -kInf ? 0.f : mn;
+    const float alpha = exp2_(m - mu);
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[kb][r] = exp2_(fmaf(p[kb][r], a.scale2, -mu));
+        sum += p[kb][r];
+      }
+    l = fmaf(l, alpha, sum);
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int st = 0; st < kRowSteps<T>; ++st) {
+        const u32x4_t pf = frag_acc<T>(p[kb], st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) Mma<T>::run(frag_cols<T, DP>(vs, 32 * kb, st, db, lane), pf, o[db]);
+      }
+  }
+  l = sum32(l);
+
+  if constexpr (SPLIT) {
+    const int64_t row = row_index(a, it.b, head, s.q0 + iq);
+    const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
+    float* po = a.part_o + (split * all + row) * a.dim;
+    store_row<float, L::DB>(o, 1.f, reinterpret_cast<char*>(po), nullptr, a.dim / 4, half, in);
+    if (in && half == 0) a.part_ml[split * all + row] = make_float2(m, l);
+    return;
+  }
+  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
+  if (!live) {
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db) o[db] = zero16();
+  }
+  char* orow = at_row_w(a.out, it.b, s.q0 + iq, head);
+  char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq, head) : nullptr;
+  store_row<T, L::DB>(o, inv, orow, rrow, dch, half, in);
+  if (in && half == 0)
+    a.lse[row_index(a, it.b, head, s.q0 + iq)] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
+  if (a.max_logits) {
+    float t = live ? top * a.scale : -kInf;
+    if (pack) {
+      if (half == 0 && t > -kInf) atomic_max_f32(a.max_logits + head, t);
+    } else {
+      t = wave_max(t);
+      if (lane == 0 && t > -kInf) atomic_max_f32(a.max_logits + head, t);
+    }
+  }
+}
+
+// Joins the splits: one wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= all) return;
+  const int i = static_cast<int>(row % a.seqs.q_tokens);
+  const int64_t bh = row / a.seqs.q_tokens;
+  const int head = static_cast<int>(bh % a.q_heads), b = static_cast<int>(bh / a.q_heads);
+  const bool live = !a.seqs.q_len || i < a.seqs.q_len[b];
+  float m = -kInf;
+  for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, a.part_ml[s * all + row].x);
+  m = wave_max(m);
+  const float mu = m == -kInf ? 0.f : m;
+  float l = 0.f;
+  for (int s = lane; s < a.splits; s += 64) {
+    const float2 v = a.part_ml[s * all + row];
+    l += v.y * exp2_(v.x - mu);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
+  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
+  char* orow = at_row_w(a.out, b, i, head);
+  char* rrow = a.res.p ? at_row_w(a.res, b, i, head) : nullptr;
+  for (int d = lane; d < a.dim; d += 64) {
+    float x = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+      const float w = exp2_(a.part_ml[s * all + row].x - mu);
+      if (w != 0.f) x = fmaf(w, a.part_o[(s * all + row) * a.dim + d], x);
+    }
+    x = live ? x * inv : 0.f;
+    const T y = from_f32<T>(x);
+    reinterpret_cast<T*>(orow)[d] = y;
+    if constexpr (sizeof(T) == 2)
+      if (rrow) reinterpret_cast<T*>(rrow)[d] = from_f32<T>(x - to_f32<T>(y));
+  }
+  if (lane == 0) {
+    a.lse[row] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
+    if (a.max_logits && live && m > -kInf) atomic_max_f32(a.max_logits + head, m * kLn2);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward.
+// ---------------------------------------------------------------------------
+// Per row: log2 of the sum of exponentials, +inf where no key is visible (so
+// that every probability recomputed from it is 0), and dout . out in fp32,
+// with what the rounding took from out where the caller kept it.  One row per
+// LPR lanes of 16 bytes.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
+  constexpr int EPC = 16 / sizeof(T), LPR = sizeof(T) == 2 ? 16 : 32;
+  const int sub = threadIdx.x % LPR;
+  const int64_t n = static_cast<int64_t>(a.seqs.batch) * a.seqs.q_tokens * a.q_heads;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
+  if (at >= n) return;
+  const int head = static_cast<int>(at % a.q_heads);
+  const int64_t bt = at / a.q_heads;
+  const int i = static_cast<int>(bt % a.seqs.q_tokens), b = static_cast<int>(bt / a.seqs.q_tokens);
+  float x = 0.f;
+  if (sub < a.dim / EPC) {
+    const u32x4_t o = *reinterpret_cast<const u32x4_t*>(at_row(a.out, b, i, head) + sub * 16);
+    const u32x4_t d = *reinterpret_cast<const u32x4_t*>(at_row(a.dout, b, i, head) + sub * 16);
+    if constexpr (sizeof(T) == 2) {
+      u32x4_t e{0, 0, 0, 0};
+      if (a.res.p) e = *reinterpret_cast<const u32x4_t*>(at_row(a.res, b, i, head) + sub * 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x = fmaf(__uint_as_float(d[k] << 16), __uint_as_float(o[k] << 16) + __uint_as_float(e[k] << 16), x);
+        x = fmaf(__uint_as_float(d[k] & 0xffff0000u),
+                 __uint_as_float(o[k] & 0xffff0000u) + __uint_as_float(e[k] & 0xffff0000u), x);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x = fmaf(__uint_as_float(d[k]), __uint_as_float(o[k]), x);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) x += __shfl_xor(x, o);
+  if (sub == 0) {
+    const int64_t row = row_index(a, b, head, i);
+    const float v = a.lse[row];
+    a.lse2[row] = v == -kInf ? kInf : v * kLog2e;
+    a.delta[row] = x;
+  }
+}
+
+// dQ: a wave holds 32 NQ queries (Q and dO rows in registers), the workgroup
+// passes over the keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
+template <typename T, int DP, int NQ, int BN>
+__global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
+  using L = Lay<T, DP>;
+  constexpr int BM = 128 * NQ, STAGE = 2 * BN * L::RB;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int dch = a.dim / L::EPC;
+  const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal);
+  const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
+  if (!s.ok) return;
+  const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
+  const int r0 = s.tile * BM + wave * 32 * NQ;
+
+  u32x4_t qf[NQ][L::STEPS], df[NQ][L::STEPS];
+  float lse2[NQ], delta[NQ];
+  int jmin[NQ], jmax[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = r0 + 32 * n + (lane & 31), iq = min(r, s.q_rows - 1);
+    load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq, head), dch, half, qf[n]);
+    load_operand<T, DP>(at_row(a.dout, it.b, s.q0 + iq, head), dch, half, df[n]);
+    const int64_t row = row_index(a, it.b, head, s.q0 + iq);
+    lse2[n] = r < s.nq ? a.lse2[row] : kInf;
+    delta[n] = a.delta[row];
+    jmax[n] = a.causal ? min(s.nk - 1, iq + shift) : s.nk - 1;
+    jmin[n] = a.causal && a.window ? max(0, iq + shift - a.window + 1) : 0;
+  }
+  const int t0q = s.tile * BM;
+  const KeyRange wg = keys_of(a, s, t0q, min(t0q + BM, s.nq) - 1);
+  const KeyRange wv = keys_of(a, s, r0, min(r0 + 32 * NQ, s.nq) - 1);
+  const int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
+
+  const uint32_t lds0 = lds_offset(smem);
+  const uint32_t kst = static_cast<uint32_t>(a.k.token), vst = static_cast<uint32_t>(a.v.token);
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (t & 1) * STAGE;
+    const int j = t * BN;
+    stage_rows<T, DP, BN>(at_row(a.k, it.b, s.k0 + j, it.kvh), kst, s.nk - j, dch, at);
+    stage_rows<T, DP, BN>(at_row(a.v, it.b, s.k0 + j, it.kvh), vst, s.nk - j, dch, at + BN * L::RB);
+  };
+  f32x16_t acc[NQ][L::DB];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db) acc[n][db] = zero16();
+  if (t0 < t1) issue(t0);
+  for (int t = t0; t < t1; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1);
+    const char* ks = smem + (t & 1) * STAGE;
+    const char* vs = ks + BN * L::RB;
+#pragma unroll
+    for (int kb = 0; kb < BN / 32; ++kb) {
+      const int j0 = t * BN + 32 * kb;
+      if (j0 >= wv.end || j0 + 32 <= wv.beg) continue;
+      f32x16_t p[NQ], d[NQ];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) p[n] = d[n] = zero16();
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st) {
+        const u32x4_t kf = frag_rows<T, DP>(ks, 32 * kb, st, lane);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) Mma<T>::run(kf, qf[n][st], p[n]);
+      }
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st) {
+        const u32x4_t vf = frag_rows<T, DP>(vs, 32 * kb, st, lane);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) Mma<T>::run(vf, df[n][st], d[n]);
+      }
+      const bool cut = j0 + 32 > wv.all_end || j0 < wv.all_beg;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if (cut) {
+          const int lo = jmin[n] - j0 - 4 * half, hi = jmax[n] - j0 - 4 * half;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 8 * (r >> 2) + (r & 3);
+            if (j < lo || j > hi) p[n][r] = -kInf;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          d[n][r] = exp2_(fmaf(p[n][r], a.scale2, -lse2[n])) * (d[n][r] - delta[n]);
+      }
+#pragma unroll
+      for (int st = 0; st < kRowSteps<T>; ++st) {
+        u32x4_t f[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) f[n] = frag_acc<T>(d[n], st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) {
+          const u32x4_t kt = frag_cols<T, DP>(ks, 32 * kb, st, db, lane);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) Mma<T>::run(kt, f[n], acc[n][db]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = r0 + 32 * n + (lane & 31), iq = min(r, s.q_rows - 1);
+    if (r >= s.nq) {
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db) acc[n][db] = zero16();
+    }
+    store_row<T, L::DB>(acc[n], a.scale, at_row_w(a.dq, it.b, s.q0 + iq, head), nullptr, dch, half, r < s.q_rows);
+  }
+}
+
+// dK, dV: a wave holds 32 NK keys (K and V rows in registers), the workgroup
+// passes over the queries of one head, or of all heads of the group:
+// S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+template <typename T, int DP, int NK, int BM>
+__global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
+  using L = Lay<T, DP>;
+  constexpr int BK = 128 * NK, DATA = 2 * BM * L::RB, STAGE = DATA + 2 * BM * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int dch = a.dim / L::EPC;
+  const Item it = item_of(blockIdx.x, a, a.kv_split ? a.group : 1, tiles, false);
+  const Seq s = find_seq(a.seqs, it.b, it.tile, BK, true);
+  if (!s.ok) return;
+  const int shift = s.nk - s.nq;
+  const int k0 = s.tile * BK, w0 = k0 + wave * 32 * NK;
+
+  u32x4_t kf[NK][L::STEPS], vf[NK][L::STEPS];
+  int qmin[NK], qmax[NK];
+#pragma unroll
+  for (int n = 0; n < NK; ++n) {
+    const int j = min(w0 + 32 * n + (lane & 31), s.k_rows - 1);
+    load_operand<T, DP>(at_row(a.k, it.b, s.k0 + j, it.kvh), dch, half, kf[n]);
+    load_operand<T, DP>(at_row(a.v, it.b, s.k0 + j, it.kvh), dch, half, vf[n]);
+    qmin[n] = a.causal ? j - shift : 0;
+    qmax[n] = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
+  }
+  // queries that see a key of the workgroup
+  int qb = 0, qe = s.nq;
+  if (a.causal) {
+    qb = max(0, k0 - shift);
+    if (a.window) qe = min(qe, min(k0 + BK, s.nk) - 1 - shift + a.window);
+  }
+  if (k0 >= s.nk) qe = 0;
+  const int t0 = qb / BM, per = max(0, (qe + BM - 1) / BM - t0);
+  const int heads = a.kv_split ? 1 : a.group, steps = per * heads;
+  const int h0 = it.kvh * a.group + (a.kv_split ? it.g : 0);
+
+  const uint32_t lds0 = lds_offset(smem);
+  const uint32_t qst = static_cast<uint32_t>(a.q.token), dst = static_cast<uint32_t>(a.dout.token);
+  auto issue = [&](int i) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (i & 1) * STAGE;
+    const int head = h0 + i / per, q = (t0 + i % per) * BM, left = s.nq - q;
+    stage_rows<T, DP, BM>(at_row(a.q, it.b, s.q0 + q, head), qst, left, dch, at);
+    stage_rows<T, DP, BM>(at_row(a.dout, it.b, s.q0 + q, head), dst, left, dch, at + BM * L::RB);
+    // the rows' statistics (queries behind the last repeat it, and are masked)
+    if (threadIdx.x < 2 * BM) {
+      const int r = threadIdx.x % BM;
+      const int64_t row = row_index(a, it.b, head, s.q0 + q + min(r, left - 1));
+      const float v = threadIdx.x < BM ? a.lse2[row] : a.delta[row];
+      *reinterpret_cast<float*>(smem + (i & 1) * STAGE + DATA + threadIdx.x * 4) = v;
+    }
+  };
+  f32x16_t dk[NK][L::DB], dv[NK][L::DB];
+#pragma unroll
+  for (int n = 0; n < NK; ++n)
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = zero16();
+  const int wk_hi = min(w0 + 32 * NK, s.nk) - 1;  // the wave's last key
+  if (steps > 0) issue(0);
+  for (int i = 0; i < steps; ++i) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (i + 1 < steps) issue(i + 1);
+    const char* qs = smem + (i & 1) * STAGE;
+    const char* os = qs + BM * L::RB;
+    const char* ss = qs + DATA;
+    const int q0 = (t0 + i % per) * BM;
+#pragma unroll
+    for (int qk = 0; qk < BM / 32; ++qk) {
+      const int q = q0 + 32 * qk;
+      if (q >= s.nq || wk_hi < w0) continue;
+      if (a.causal && q + 31 + shift < w0) continue;
+      if (a.causal && a.window && q + shift - wk_hi >= a.window) continue;
+      const bool cut = q + 32 > s.nq || (a.causal && q + shift < w0 + 32 * NK - 1) ||
+                       (a.causal && a.window && q + 31 + shift - w0 >= a.window);
+      f32x16_t p[NK], d[NK];
+#pragma unroll
+      for (int n = 0; n < NK; ++n) p[n] = d[n] = zero16();
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st) {
+        const u32x4_t f = frag_rows<T, DP>(qs, 32 * qk, st, lane);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) Mma<T>::run(f, kf[n][st], p[n]);
+      }
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st) {
+        const u32x4_t f = frag_rows<T, DP>(os, 32 * qk, st, lane);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) Mma<T>::run(f, vf[n][st], d[n]);
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 ls = *reinterpret_cast<const float4*>(ss + (32 * qk + 8 * g + 4 * half) * 4);
+        const float4 de = *reinterpret_cast<const float4*>(ss + (BM + 32 * qk + 8 * g + 4 * half) * 4);
+        const float lv[4] = {ls.x, ls.y, ls.z, ls.w}, dl[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = p[n][4 * g + e];
+            if (cut) {
+              const int qq = q + 8 * g + 4 * half + e;
+              if (qq < qmin[n] || qq > qmax[n]) x = -kInf;
+            }
+            x = exp2_(fmaf(x, a.scale2, -lv[e]));
+            p[n][4 * g + e] = x;
+            d[n][4 * g + e] = x * (d[n][4 * g + e] - dl[e]);
+          }
+      }
+#pragma unroll
+      for (int st = 0; st < kRowSteps<T>; ++st) {
+        u32x4_t f[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(p[n], st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) {
+          const u32x4_t x = frag_cols<T, DP>(os, 32 * qk, st, db, lane);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dv[n][db]);
+        }
+      }
+#pragma unroll
+      for (int st = 0; st < kRowSteps<T>; ++st) {
+        u32x4_t f[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(d[n], st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) {
+          const u32x4_t x = frag_cols<T, DP>(qs, 32 * qk, st, db, lane);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dk[n][db]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NK; ++n) {
+    const int r = w0 + 32 * n + (lane & 31), j = min(r, s.k_rows - 1);
+    if (r >= s.nk) {
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = zero16();
+    }
+    const bool on = r < s.k_rows;
+    if (a.kv_split) {
+      const int64_t row = (static_cast<int64_t>(it.b) * a.seqs.k_tokens + s.k0 + j) * a.q_heads + h0;
+      store_row<float, L::DB>(dk[n], a.scale, reinterpret_cast<char*>(a.part_dk + row * a.dim), nullptr, a.dim / 4,
+                              half, on);
+      store_row<float, L::DB>(dv[n], 1.f, reinterpret_cast<char*>(a.part_dv + row * a.dim), nullptr, a.dim / 4,
+                              half, on);
+    } else {
+      store_row<T, L::DB>(dk[n], a.scale, at_row_w(a.dk, it.b, s.k0 + j, it.kvh), nullptr, dch, half, on);
+      store_row<T, L::DB>(dv[n], 1.f, at_row_w(a.dv, it.b, s.k0 + j, it.kvh), nullptr, dch, half, on);
+    }
+  }
+}
+
+// Sums the heads of each group, in order: a thread has 4 elements of dk or dv.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
+  const int quads = a.dim / 4;
+  const int64_t n = static_cast<int64_t>(a.seqs.batch) * a.seqs.k_tokens * a.kv_heads * quads;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (at >= 2 * n) return;
+  const bool second = at >= n;
+  const int64_t i = second ? at - n : at;
+  const int quad = static_cast<int>(i % quads);
+  const int64_t kh = i / quads, tok = kh / a.kv_heads;
+  const int head = static_cast<int>(kh % a.kv_heads);
+  const int b = static_cast<int>(tok / a.seqs.k_tokens), j = static_cast<int>(tok % a.seqs.k_tokens);
+  if (a.seqs.q_off) {  // rows behind the last sequence stay as they are
+    if (j < a.seqs.k_off[0] || j >= a.seqs.k_off[a.seqs.n_seq]) return;
+  }
+  const float* p = (second ? a.part_dv : a.part_dk) + (tok * a.q_heads + static_cast<int64_t>(head) * a.group) * a.dim + 4 * quad;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int g = 0; g < a.group; ++g, p += a.dim) {
+    const float4 y = *reinterpret_cast<const float4*>(p);
+    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+  }
+  char* row = at_row_w(second ? a.dv : a.dk, b, j, head);
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(row + quad * 8) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+  else
+    *reinterpret_cast<float4*>(row + quad * 16) = x;
+}
+
+// ---------------------------------------------------------------------------
+// Rotary positions.  A workgroup takes a few tokens: their angles once (fp64
+// product and reduction to a fraction of a turn, then fp32 sine and cosine),
+// through LDS to every head.  HBM-bound: each element is read and written
+// once.
+// ---------------------------------------------------------------------------
+constexpr int kRotPairs = 512;  // angles of a workgroup
+template <typename T>
+__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int per_block) {
+  constexpr int EPC = 16 / sizeof(T);
+  __shared__ float2 turn[kRotPairs];
+  const int half = a.rot / 2;
+  const int64_t all = a.batch * a.tokens, first = static_cast<int64_t>(blockIdx.x) * per_block;
+  const int n = static_cast<int>(min(static_cast<int64_t>(per_block), all - first));
+  for (int i = threadIdx.x; i < n * half; i += 256) {
+    const int64_t tok = first + i / half, b = tok / a.tokens, t = tok % a.tokens;
+    int64_t pos = t;
+    if (a.positions) {
+      const int64_t at = b * a.pos_batch + t * a.pos_token;
+      pos = a.positions64 ? static_cast<const int64_t*>(a.positions)[at] : static_cast<const int32_t*>(a.positions)[at];
+    }
+    const double rev = static_cast<double>(pos + a.first) * (a.freqs[i % half] * 0.15915494309189533577);
+    float sn, cs;
+    sincospif(static_cast<float>(2.0 * (rev - rint(rev))), &sn, &cs);
+    turn[i] = make_float2(cs * a.scale, sn * a.scale * a.sign);
+  }
+  __syncthreads();
+  for (int k = 0; k < a.n; ++k) {
+    const RotaryTensor& t = a.t[k];
+    const bool vec = t.vec != 0, same = t.x.p == t.y.p;
+    // units of a head: pieces that turn, then pieces that are copied
+    const int width = vec ? EPC : 1;
+    const int turning = (a.interleaved ? a.rot / (vec ? EPC : 2) : half / width);
+    const int units = turning + (same ? 0 : (a.dim - a.rot) / width);
+    const int total = n * t.heads * units;
+    for (int i = threadIdx.x; i < total; i += 256) {
+      const int u = i % units, th = i / units, head = th % t.heads, tk = th / t.heads;
+      const int64_t tok = first + tk, b = tok / a.tokens, at = tok % a.tokens;
+      const T* x = reinterpret_cast<const T*>(t.x.p + b * t.x.batch + at * t.x.token + head * t.x.head);
+      T* y = reinterpret_cast<T*>(t.y.p + b * t.y.batch + at * t.y.token + head * t.y.head);
+      const float2* w = turn + tk * half;
+      if (u >= turning) {
+        const int d = a.rot + (u - turning) * width;
+        if (vec) *reinterpret_cast<u32x4_t*>(y + d) = *reinterpret_cast<const u32x4_t*>(x + d);
+        else y[d] = x[d];
+      } else if (!vec) {
+        const int p = a.interleaved ? 2 * u : u, q = a.interleaved ? p + 1 : u + half;
+        const float c = w[u].x, sn = w[u].y, e = to_f32<T>(x[p]), f = to_f32<T>(x[q]);
+        y[p] = from_f32<T>(e * c - f * sn);
+        y[q] = from_f32<T>(e * sn + f * c);
+      } else {
+        // a piece of EPC elements: pairs of it (interleaved), or it and the
+        // piece half a rotation further
+        float e[8], f[8];
+        if constexpr (sizeof(T) == 2) load8(x, u * EPC, e);
+        else *reinterpret_cast<float4*>(e) = *reinterpret_cast<const float4*>(x + u * EPC);
+        if (a.interleaved) {
+#pragma unroll
+          for (int q = 0; q < EPC / 2; ++q) {
+            const float2 cw = w[u * (EPC / 2) + q];
+            const float g = e[2 * q], h = e[2 * q + 1];
+            e[2 * q] = g * cw.x - h * cw.y;
+            e[2 * q + 1] = g * cw.y + h * cw.x;
+          }
+        } else {
+          if constexpr (sizeof(T) == 2) load8(x, u * EPC + half, f);
+          else *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(x + u * EPC + half);
+#pragma unroll
+          for (int q = 0; q < EPC; ++q) {
+            const float2 cw = w[u * EPC + q];
+            const float g = e[q], h = f[q];
+            e[q] = g * cw.x - h * cw.y;
+            f[q] = g * cw.y + h * cw.x;
+          }
+          if constexpr (sizeof(T) == 2) store8(y, u * EPC + half, f);
+          else *reinterpret_cast<float4*>(y + u * EPC + half) = *reinterpret_cast<const float4*>(f);
+        }
+        if constexpr (sizeof(T) == 2) store8(y, u * EPC, e);
+        else *reinterpret_cast<float4*>(y + u * EPC) = *reinterpret_cast<const float4*>(e);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The clip.  A workgroup has kClipRows rows of one weight; rows whose factor is
+// 1 are not touched.  HBM-bound on the rows that change.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float clip_gamma(float m, float threshold) {
+  return m > threshold && m < kInf ? threshold / m : 1.f;
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_qk_clip(ClipArgs a) {
+  constexpr int EPC = 16 / sizeof(T);
+  int k = 0;
+  while (k + 1 < a.n && a.first[k + 1] <= static_cast<int>(blockIdx.x)) ++k;
+  const ClipEntry& e = a.e[k];
+  const int lane = threadIdx.x & 63, group = e.q_heads / e.kv_heads;
+  const int rows_q = e.q_heads * e.dim, rows = rows_q + e.kv_heads * e.dim;
+  const int base = (blockIdx.x - a.first[k]) * kClipRows;
+  for (int i = threadIdx.x >> 6; i < kClipRows; i += 4) {
+    const int row = base + i;
+    if (row >= rows) return;
+    const bool is_q = row < rows_q;
+    const int at = is_q ? row : row - rows_q, head = at / e.dim, kvh = is_q ? head / group : head;
+    float least = 1.f;
+    for (int g = 0; g < group; ++g) least = fminf(least, clip_gamma(e.logits[kvh * group + g], e.threshold));
+    const float key = sqrtf(least);
+    const float f = is_q ? clip_gamma(e.logits[head], e.threshold) / key : key;
+    if (f == 1.f) continue;
+    T* w = reinterpret_cast<T*>(is_q ? e.wq + at * e.ldq : e.wk + at * e.ldk);
+    int done = 0;
+    if (e.vec) {
+      done = e.cols / EPC * EPC;
+      for (int c = lane * EPC; c < done; c += 64 * EPC) {
+        float x[8];
+        if constexpr (sizeof(T) == 2) {
+          load8(w, c, x);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] *= f;
+          store8(w, c, x);
+        } else {
+          float4 v = *reinterpret_cast<const float4*>(w + c);
+          v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+          *reinterpret_cast<float4*>(w + c) = v;
+        }
+      }
+    }
+    for (int c = done + lane; c < e.cols; c += 64) w[c] = from_f32<T>(to_f32<T>(w[c]) * f);
+  }
+}
+__global__ __launch_bounds__(256) void k_reset_logits(ClipArgs a) {
+  const ClipEntry& e = a.e[blockIdx.x];
+  for (int i = threadIdx.x; i < e.q_heads; i += 256) e.logits[i] = -kInf;
+}
+
+// Tiles of `bt` tokens: exactly per sequence (dense), or as many as packed
+// sequences can have.
+int64_t tiles_of(const Seqs& s, int64_t tokens, int bt) {
+  return (tokens + bt - 1) / bt + (s.q_off ? s.n_seq : 0);
+}
+double pairs_of(const AttnArgs& a) {  // of a dense request, as an upper bound for packed ones
+  const double nq = a.seqs.q_tokens, nk = a.seqs.k_tokens;
+  return double(a.seqs.batch) * a.q_heads * nq * nk * (a.causal ? 0.5 : 1.0);
+}
+
+// One tile of rows holds every query of every head of a group.
+bool packs_heads(const Seqs& s, int group) {
+  return !s.q_off && group > 1 && int64_t(s.q_tokens) * group <= 128;
+}
+
+template <typename T, int DP, int BN>
+hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
+  const bool pack = packs_heads(a.seqs, a.group);
+  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128);
+  const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
+  const dim3 g(static_cast<unsigned>(grid)), b(256);
+  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
+  else hipLaunchKernelGGL((k_attn_fwd<T, DP, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
+  hipLaunchKernelGGL((k_attn_join<T>), dim3(static_cast<unsigned>((rows + 3) / 4)), b, 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename T, int DP, int NB, int TILE>
+hipError_t backward_of(const AttnArgs& a, hipStream_t st) {
+  constexpr int LPR = sizeof(T) == 2 ? 16 : 32;
+  const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
+  const dim3 b(256);
+  hipError_t e;
+  if (rows > 0) {
+    const int64_t per = 256 / LPR;
+    hipLaunchKernelGGL((k_attn_delta<T>), dim3(static_cast<unsigned>((rows + per - 1) / per)), b, 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 * NB);
+    hipLaunchKernelGGL((k_attn_dq<T, DP, NB, TILE>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
+                       st, a, int(tiles));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.seqs.k_tokens == 0) return hipSuccess;
+  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 * NB);
+  const int64_t grid = a.seqs.batch * a.kv_heads * (a.kv_split ? a.group : 1) * tiles;
+  hipLaunchKernelGGL((k_attn_dkv<T, DP, NB, TILE>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
+  if ((e = hipGetLastError()) != hipSuccess || !a.kv_split) return e;
+  const int64_t n = 2 * a.seqs.batch * int64_t(a.seqs.k_tokens) * a.kv_heads * (a.dim / 4);
+  hipLaunchKernelGGL((k_attn_sum_heads<T>), dim3(static_cast<unsigned>((n + 255) / 256)), b, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype, bool causal, int window) {
+  if (s.q_off || (causal && window)) return 1;
+  const bool pack = packs_heads(s, q_heads / kv_heads);
+  const int64_t items = s.batch * (pack ? int64_t(kv_heads) : q_heads * tiles_of(s, s.q_tokens, 128));
+  if (items == 0 || items >= 256) return 1;
+  // four tiles of keys at least in each part
+  const int64_t parts = std::min<int64_t>(512 / items, s.k_tokens / 256);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
+}
+
+bool backward_splits_heads(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype) {
+  return q_heads != kv_heads;
+}
+
+hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+  if (a.seqs.batch * a.seqs.q_tokens == 0) return hipSuccess;
+  Timed tm(timer, KK_ATTENTION_FWD, st);
+  hipError_t e;
+  if (dtype == DT_BF16) e = a.dim <= 64 ? forward_of<uint16_t, 64, 64>(a, st) : forward_of<uint16_t, 128, 64>(a, st);
+  else e = a.dim <= 64 ? forward_of<float, 64, 64>(a, st) : forward_of<float, 128, 32>(a, st);
+  const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
+  if (e == hipSuccess)
+    tm.done(4.0 * pairs_of(a) * a.dim, 0,
+            b * a.dim * es * 2.0 * (double(a.seqs.q_tokens) * a.q_heads + double(a.seqs.k_tokens) * a.kv_heads));
+  return e;
+}
+
+hipError_t run_attention_backward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+  if (a.seqs.batch == 0) return hipSuccess;
+  Timed tm(timer, KK_ATTENTION_BWD, st);
+  hipError_t e;
+  if (dtype == DT_BF16) e = a.dim <= 64 ? backward_of<uint16_t, 64, 2, 64>(a, st) : backward_of<uint16_t, 128, 2, 64>(a, st);
+  else e = a.dim <= 64 ? backward_of<float, 64, 1, 32>(a, st) : backward_of<float, 128, 1, 32>(a, st);
+  const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
+  if (e == hipSuccess)
+    tm.done(10.0 * pairs_of(a) * a.dim, 0,
+            b * a.dim * es * 4.0 * (double(a.seqs.q_tokens) * a.q_heads + double(a.seqs.k_tokens) * a.kv_heads));
+  return e;
+}
+
+hipError_t run_rotary(const RotaryArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+  const int64_t all = a.batch * a.tokens;
+  if (all == 0) return hipSuccess;
+  Timed tm(timer, KK_ROTARY, st);
+  // a few tokens a workgroup, fewer where that leaves compute units idle
+  int per = std::max(1, std::min(8, kRotPairs / std::max(1, a.rot / 2)));
+  while (per > 1 && (all + per - 1) / per < 1024) per /= 2;
+  const dim3 g(static_cast<unsigned>((all + per - 1) / per)), b(256);
+  if (dtype == DT_BF16) hipLaunchKernelGGL((k_rotary<uint16_t>), g, b, 0, st, a, per);
+  else hipLaunchKernelGGL((k_rotary<float>), g, b, 0, st, a, per);
+  const hipError_t e = hipGetLastError();
+  double heads = 0;
+  for (int i = 0; i < a.n; ++i) heads += a.t[i].heads;
+  if (e == hipSuccess) tm.done(0, 0, 2.0 * double(all) * heads * a.dim * (dtype == DT_BF16 ? 2 : 4));
+  return e;
+}
+
+hipError_t run_qk_clip(const ClipArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+  if (a.n == 0 || a.first[a.n] == 0) return hipSuccess;
+  Timed tm(timer, KK_QK_CLIP, st);
+  const dim3 g(static_cast<unsigned>(a.first[a.n])), b(256);
+  if (dtype == DT_BF16) hipLaunchKernelGGL((k_qk_clip<uint16_t>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((k_qk_clip<float>), g, b, 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) tm.done(0, 0, 0);
+  return e;
+}
+
+hipError_t run_reset_logits(const ClipArgs& a, hipStream_t st) {
+  if (a.n == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_reset_logits, dim3(a.n), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace muon

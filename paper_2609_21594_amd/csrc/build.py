@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libmuon_hip.so")
-SOURCES = ["muon_api.hip", "muon_kernels.hip"]
+SOURCES = ["muon_api.hip", "muon_kernels.hip", "attention_api.hip", "attention_kernels.hip"]
 ARCH = os.environ.get("MUON_HIP_ARCH", "gfx950")
 
 

@@ -1236,6 +1236,68 @@ bool bytes_meet(uintptr_t a, uintptr_t na, uintptr_t b, uintptr_t nb) { return a
 
 }  // namespace
 
+namespace muon {
+
+int handle_device(muon_handle* h) { return h->device; }
+LaunchTimer* handle_timer(muon_handle* h) { return h->profiling ? &h->timer : nullptr; }
+void handle_error(muon_handle* h, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(h->err, sizeof h->err, fmt, ap);
+  va_end(ap);
+}
+void handle_clear_error(muon_handle* h) { h->err[0] = '\0'; }
+
+bool extents_on_device(muon_handle* h, const Extent* e, size_t n) {
+  for (size_t i = 0; i < n; ++i) {
+    const Span s{e[i].lo, e[i].hi};
+    if (check_device_spans(h, &s, 1) != MUON_OK) return false;
+  }
+  return true;
+}
+
+// Most calls pass separate buffers: their hulls settle it.  Interleaved ones
+// (slices of one tensor) are compared run by run.
+bool buffers_disjoint(const Strided* b, size_t n) {
+  const auto hull = [](const Strided& x) {
+    uintptr_t hi = x.lo + uintptr_t(x.len);
+    for (int k = 0; k < 3; ++k) hi += uintptr_t(x.count[k] - 1) * uintptr_t(x.stride[k]);
+    return hi;
+  };
+  bool meet = false;
+  for (size_t i = 0; i < n && !meet; ++i)
+    for (size_t j = i + 1; j < n && !meet; ++j)
+      meet = (b[i].written || b[j].written) && b[i].lo < hull(b[j]) && b[j].lo < hull(b[i]);
+  if (!meet) return true;
+  std::vector<Run> runs;
+  for (size_t i = 0; i < n; ++i) {
+    // levels in order of their stride; a read-only one that repeats or
+    // overlaps itself is taken as its hull
+    int order[3] = {0, 1, 2};
+    const Strided& x = b[i];
+    std::sort(order, order + 3, [&](int p, int q) { return x.stride[p] < x.stride[q]; });
+    int64_t st[3], ct[3], span = x.len;
+    bool nested = true;
+    int m = 0;
+    for (int k : order) {
+      if (x.count[k] == 1) continue;
+      nested = nested && x.stride[k] >= span;
+      st[m] = x.stride[k];
+      ct[m++] = x.count[k];
+      span += x.stride[k] * (x.count[k] - 1);
+    }
+    for (; m < 3; ++m) { st[m] = span; ct[m] = 1; }
+    if (!nested) {
+      runs.push_back({x.lo, uintptr_t(span), uintptr_t(span), 1, x.written});
+      continue;
+    }
+    view_runs(x.lo, 1, ct[0] * ct[1], x.len, ct[2], st[0], ct[0], st[1], st[2], x.written, runs);
+  }
+  return runs_disjoint(runs);
+}
+
+}  // namespace muon
+
 extern "C" {
 
 int muon_abi_version(void) { return MUON_HIP_ABI_VERSION; }
@@ -1360,7 +1422,8 @@ muon_status_t muon_profile_read(muon_handle_t h, muon_kernel_stats_t* out, int c
                                 int reset) {
   static const char* const kNames[muon::KK_COUNT] = {
       "momentum_norm", "norm_finalize", "rescale", "gram_syrk",
-      "poly_syrk", "update_gemm", "update_apply_gemm", "apply_x0", "adamw", "ns_small"};
+      "poly_syrk", "update_gemm", "update_apply_gemm", "apply_x0", "adamw", "ns_small",
+      "rotary", "attention_forward", "attention_backward", "qk_clip"};
   if (!h || (cap > 0 && !out)) return MUON_ERR_INVALID_ARGUMENT;
   DeviceGuard dg(h->device);
   const bool ok = h->timer.collect();

@@ -8,6 +8,8 @@
 
 #include <string>
 
+struct muon_handle;
+
 namespace muon {
 
 // Workspace extents of every matrix are rounded up to this multiple, and the
@@ -92,7 +94,7 @@ struct StepScalars {
 // Kernel families, for the optional per-launch timing.
 enum KernelKind : int {
   KK_PARTIALS = 0, KK_FINALIZE, KK_NORMALIZE, KK_GRAM, KK_POLY, KK_UPDATE, KK_FINAL,
-  KK_APPLY_X0, KK_ADAMW, KK_SMALL, KK_COUNT
+  KK_APPLY_X0, KK_ADAMW, KK_SMALL, KK_ROTARY, KK_ATTENTION_FWD, KK_ATTENTION_BWD, KK_QK_CLIP, KK_COUNT
 };
 
 // Receives a bracket around every launch when timing is enabled.
@@ -258,5 +260,28 @@ std::string route_of(const ChunkGeom& g, int K);
 hipError_t run_chunk(const ChunkGeom& g, const MatDesc* d_desc, const ChunkBuffers& wb,
                      const StepScalars& sc, const float* coeffs /* host, K x 3 */, int K,
                      hipStream_t stream, LaunchTimer* timer /* may be null */);
+
+// ---------------------------------------------------------------------------
+// Services of muon_api.hip for entry points in other files.
+// ---------------------------------------------------------------------------
+// Bytes [lo, hi) of a buffer.
+struct Extent { uintptr_t lo, hi; };
+// A strided buffer: levels of (stride in bytes, count), innermost first, around
+// `len` contiguous bytes.  Only a written one needs levels that do not overlap.
+struct Strided {
+  uintptr_t lo;
+  int64_t len;
+  int64_t stride[3], count[3];
+  bool written;
+};
+int handle_device(muon_handle* h);
+LaunchTimer* handle_timer(muon_handle* h);  // null unless profiling
+void handle_error(muon_handle* h, const char* fmt, ...);
+void handle_clear_error(muon_handle* h);
+// Whether every extent is device memory of the handle's device; the message is
+// set where not.
+bool extents_on_device(muon_handle* h, const Extent* e, size_t n);
+// Whether no written buffer meets another one.
+bool buffers_disjoint(const Strided* b, size_t n);
 
 }  // namespace muon
