@@ -368,9 +368,9 @@ typedef struct {
 /* Scratch bytes of a forward (backward = 0) or backward (1) pass: host only,
  * from the sizes alone (no pointer is looked at).  0 is possible. */
 muon_status_t muon_attention_scratch(const muon_attention_t* a, int backward, size_t* bytes);
-/* Host-only checks of a forward (g NULL) or backward request: the status that
- * the launching call would return before it asks the runtime about buffers;
- * the reason goes into msg (may be NULL). */
+/* Host-only checks of a forward (g NULL) or backward request, of a rotation
+ * and of a clip: the status that the launching call would return before it
+ * asks the runtime about buffers; the reason goes into msg (may be NULL). */
 muon_status_t muon_validate_attention(const muon_attention_t* a, const muon_attention_grad_t* g, char* msg,
                                       size_t msg_len);
 /* Writes out, lse, residual (if given) and max_logits (if given). */
@@ -409,6 +409,8 @@ typedef struct {
 /* Tensors may have any element alignment here (16-byte aligned ones with
  * rotary_dim a multiple of 16 in bf16, of 8 in fp32, are faster). */
 muon_status_t muon_rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_tensor_t* tensors, void* stream);
+muon_status_t muon_validate_rotary(const muon_rotary_t* r, const muon_rotary_tensor_t* tensors, char* msg,
+                                   size_t msg_len);
 
 /* QK-clip of n pairs of weights.  wq is [q_heads * head_dim][cols], wk
  * [kv_heads * head_dim][cols], row strides q_ld and k_ld (elements, 0 = cols).
@@ -429,6 +431,7 @@ typedef struct {
   int32_t reserved;        /* must be 0 */
 } muon_qk_clip_t;
 muon_status_t muon_qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n, int reset, void* stream);
+muon_status_t muon_validate_qk_clip(const muon_qk_clip_t* entries, int64_t n, char* msg, size_t msg_len);
 
 /* Host-only checks and planning (no device needed).  muon_validate_step
  * returns the status muon_step would return for these arguments before

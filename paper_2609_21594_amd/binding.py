@@ -122,7 +122,8 @@ EXPORTS = ["muon_create", "muon_destroy", "muon_reserve", "muon_set_workspace_li
            "muon_abi_version", "muon_profile_enable", "muon_profile_read", "muon_adamw_step",
            "muon_set_streams", "ns_orthogonalize_batched_noalloc", "muon_stream_copy",
            "muon_attention_scratch", "muon_validate_attention", "muon_attention_forward",
-           "muon_attention_backward", "muon_rotary", "muon_qk_clip"]
+           "muon_attention_backward", "muon_rotary", "muon_qk_clip", "muon_validate_rotary",
+           "muon_validate_qk_clip"]
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -172,8 +173,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.muon_attention_backward.argtypes = [vp, vp, vp, vp]
     lib.muon_rotary.argtypes = [vp, vp, vp, vp]
     lib.muon_qk_clip.argtypes = [vp, vp, i64, ctypes.c_int, vp]
+    lib.muon_validate_rotary.argtypes = [vp, vp, ctypes.c_char_p, ctypes.c_size_t]
+    lib.muon_validate_qk_clip.argtypes = [vp, i64, ctypes.c_char_p, ctypes.c_size_t]
     for name in ("muon_attention_scratch", "muon_validate_attention", "muon_attention_forward",
-                 "muon_attention_backward", "muon_rotary", "muon_qk_clip"):
+                 "muon_attention_backward", "muon_rotary", "muon_qk_clip", "muon_validate_rotary",
+                 "muon_validate_qk_clip"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("muon_create", "muon_destroy", "muon_reserve", "muon_set_workspace_limit",
                  "muon_step", "ns_orthogonalize_batched", "muon_validate_step", "muon_plan_step",
@@ -384,7 +388,7 @@ _NO_HEADS = (0, 0, 0, 0)
 def _heads(t):
     """(pointer, batch stride, token stride, head stride) of [B, S, H, D] or [S, H, D]."""
     st = t.stride()
-    if t.shape[-1] > 1 and st[-1] != 1:
+    if st[-1] != 1 and t.shape[-1] > 1 and t.numel():
         raise ValueError("the elements of a head must be contiguous")
     return (t.data_ptr(), st[0], st[1], st[2]) if len(st) == 4 else (t.data_ptr(), 0, st[0], st[1])
 
@@ -440,6 +444,37 @@ class _Attention:
 def _expect(t, shape, dtype, what):
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+
+
+def clip_records(wqs, wks, max_logits, threshold) -> bytes:
+    """Packed entries of muon_qk_clip, their shapes checked (host only)."""
+    import torch
+    recs = []
+    for i, (q, k, m) in enumerate(zip(wqs, wks, max_logits)):
+        if q.dim() != 2 or k.dim() != 2 or q.shape[1] != k.shape[1] or q.dtype != k.dtype:
+            raise ValueError(f"entry {i}: weights must be matrices of one dtype and one number of columns")
+        if m.dtype != torch.float32 or m.dim() != 1 or not m.is_contiguous() or m.numel() < 1:
+            raise TypeError(f"entry {i}: logits must be a contiguous 1-D float32 tensor")
+        hq, (rows, cols) = m.numel(), q.shape
+        hd = rows // hq
+        if rows % hq or hd == 0 or k.shape[0] % hd or k.shape[0] == 0:
+            raise ValueError(f"entry {i}: {rows} query rows and {k.shape[0]} key rows are not whole heads of {hq}")
+        for t in (q, k):
+            if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
+                raise ValueError(f"entry {i}: rows must be contiguous and distinct")
+        recs.append(_CLIP_PACK.pack(q.data_ptr(), k.data_ptr(), m.data_ptr(), q.stride(0) if rows > 1 else cols,
+                                    k.stride(0) if k.shape[0] > 1 else cols, cols, hq, k.shape[0] // hd, hd,
+                                    _dtype_code(q), float(threshold), 0))
+    return b"".join(recs)
+
+
+def validate_qk_clip(wqs, wks, max_logits, threshold):
+    """Host-only checks of a clip: raises where `Muon.qk_clip` would."""
+    lib = load_library()
+    msg = ctypes.create_string_buffer(256)
+    st = lib.muon_validate_qk_clip(clip_records(wqs, wks, max_logits, threshold), len(wqs), msg, 256)
+    if st != MUON_OK:
+        raise MuonError(st, msg.value.decode())
 
 
 class Muon:
@@ -735,30 +770,14 @@ class Muon:
         key weights wks[i] [Hkv * hd, cols] so that every head whose largest
         logit max_logits[i] (fp32, [Hq]) exceeds `threshold` comes down to it
         (muon_qk_clip).  reset: the logits become -inf afterwards."""
-        import torch
         n = len(wqs)
         if not (len(wks) == len(max_logits) == n):
             raise ValueError("query weights, key weights and logits must have equal length")
         _check_device([*wqs, *wks, *max_logits], self.device)
-        recs = []
-        for i, (q, k, m) in enumerate(zip(wqs, wks, max_logits)):
-            if q.dim() != 2 or k.dim() != 2 or q.shape[1] != k.shape[1] or q.dtype != k.dtype:
-                raise ValueError(f"entry {i}: weights must be matrices of one dtype and one number of columns")
-            if m.dtype != torch.float32 or m.dim() != 1 or not m.is_contiguous() or m.numel() < 1:
-                raise TypeError(f"entry {i}: logits must be a contiguous 1-D float32 tensor")
-            hq, (rows, cols) = m.numel(), q.shape
-            hd = rows // hq
-            if rows % hq or hd == 0 or k.shape[0] % hd or k.shape[0] == 0:
-                raise ValueError(f"entry {i}: {rows} query rows and {k.shape[0]} key rows are not whole heads of {hq}")
-            for t in (q, k):
-                if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
-                    raise ValueError(f"entry {i}: rows must be contiguous and distinct")
-            recs.append(_CLIP_PACK.pack(q.data_ptr(), k.data_ptr(), m.data_ptr(), q.stride(0) if rows > 1 else cols,
-                                        k.stride(0) if k.shape[0] > 1 else cols, cols, hq, k.shape[0] // hd, hd,
-                                        _dtype_code(q), float(threshold), 0))
+        recs = clip_records(wqs, wks, max_logits, threshold)
         ptr, ctx = self._on(stream)
         with ctx:
-            self._check(self.lib.muon_qk_clip(self.h, b"".join(recs), n, int(bool(reset)), ptr))
+            self._check(self.lib.muon_qk_clip(self.h, recs, n, int(bool(reset)), ptr))
 
 
 def validate_step(entries: Sequence[MuonParam], hp: MuonHParams):

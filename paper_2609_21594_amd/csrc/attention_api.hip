@@ -307,77 +307,68 @@ muon_status_t guarded(muon_handle_t h, F&& f) {
   }
 }
 
-muon_status_t rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_tensor_t* t, void* stream) {
-  muon::handle_clear_error(h);
-  Why why;
-  muon::RotaryArgs k{};
-  Strided bufs[2 * muon::kRotaryMax + 2];
-  Extent ext[2 * muon::kRotaryMax + 2];
-  size_t nb = 0, ne = 0;
-  const auto check = [&]() -> muon_status_t {
-    if (!r || !t) return why.invalid("the request is NULL");
-    if (!known_dtype(r->dtype)) return why.invalid("unknown dtype");
-    if (r->n_tensors < 1 || r->n_tensors > muon::kRotaryMax) return why.invalid("1 to %d tensors a call", muon::kRotaryMax);
-    if (r->head_dim < 1) return why.invalid("head_dim must be >= 1");
-    if (r->head_dim > kMaxRotaryDim) return why.fail(MUON_ERR_UNSUPPORTED, "head_dim %d: at most %d", r->head_dim, kMaxRotaryDim);
-    if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > r->head_dim)
-      return why.invalid("rotary_dim must be even, 2 to head_dim");
-    if (r->layout != 0 && r->layout != 1) return why.invalid("layout must be 0 (halves) or 1 (neighbours)");
-    if (r->inverse != 0 && r->inverse != 1) return why.invalid("inverse must be 0 or 1");
-    if (!std::isfinite(r->scale)) return why.invalid("scale must be finite");
-    if (r->batch < 0 || r->tokens < 0 || r->batch > kMaxTokens || r->tokens > kMaxTokens)
-      return why.invalid("batch or tokens out of range");
-    if (double(r->batch) * double(r->tokens) >= double(1 << 24))  // a token a workgroup at the least
-      return why.fail(MUON_ERR_UNSUPPORTED, "too many tokens in one call (at most 2^24)");
-    const int64_t es = elem_size(r->dtype), all = r->batch * r->tokens;
-    if (all == 0) return MUON_OK;
-    if (!r->freqs) return why.invalid("freqs is NULL");
-    if (reinterpret_cast<uintptr_t>(r->freqs) % 8) return why.invalid("freqs is not 8-byte aligned");
-    bufs[nb++] = flat(r->freqs, r->rotary_dim * 4, false);
-    ext[ne++] = extent(r->freqs, r->rotary_dim * 4);
-    if (r->positions) {
-      const int64_t ps = r->positions_int64 ? 8 : 4;
-      if (reinterpret_cast<uintptr_t>(r->positions) % uintptr_t(ps)) return why.invalid("positions are not aligned to their size");
-      const int64_t bs = r->batch > 1 ? r->position_batch_stride : 0, ts = r->tokens > 1 ? r->position_token_stride : 0;
-      if (bs < 0 || ts < 0 || bs > (int64_t(1) << 40) || ts > (int64_t(1) << 24)) return why.invalid("positions: stride out of range");
-      if (bs > 0 && r->batch > (int64_t(1) << 46) / bs) return why.invalid("positions: extent out of range");
-      const int64_t span = ((r->batch - 1) * bs + (r->tokens - 1) * ts + 1) * ps;
-      bufs[nb++] = flat(r->positions, span, false);
-      ext[ne++] = extent(r->positions, span);
-      k.pos_batch = bs;
-      k.pos_token = ts;
-    }
-    const int half = r->rotary_dim / 2, unit = int(16 / es);
-    for (int i = 0; i < r->n_tensors; ++i) {
-      View x, y;
-      if (t[i].heads < 0 || t[i].heads > 65536) return why.invalid("tensor %d: heads out of range", i);
-      const bool same = t[i].x.data == t[i].y.data;
-      if (same && (t[i].x.batch_stride != t[i].y.batch_stride || t[i].x.token_stride != t[i].y.token_stride ||
-                   t[i].x.head_stride != t[i].y.head_stride))
-        return why.invalid("tensor %d: in place, x and y must have the same strides", i);
-      muon_status_t st = make_view(t[i].x, "x", r->batch, r->tokens, t[i].heads, r->head_dim, es, es, same, x, why);
-      if (st != MUON_OK) return st;
-      if ((st = make_view(t[i].y, "y", r->batch, r->tokens, t[i].heads, r->head_dim, es, es, true, y, why)) != MUON_OK) return st;
-      const auto by16 = [](const Heads& v) {
-        return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.batch % 16 == 0 && v.token % 16 == 0 && v.head % 16 == 0;
-      };
-      k.t[i].x = x.h;
-      k.t[i].y = y.h;
-      k.t[i].heads = int32_t(t[i].heads);
-      k.t[i].vec = by16(x.h) && by16(y.h) && r->head_dim % unit == 0 &&
-                   (r->layout == 1 ? r->rotary_dim : half) % unit == 0;
-      if (t[i].heads == 0) continue;
-      if (!same) { bufs[nb++] = x.s; ext[ne++] = x.e; }
-      bufs[nb++] = y.s;
-      ext[ne++] = y.e;
-    }
-    if (!muon::buffers_disjoint(bufs, nb)) return why.invalid("an output overlaps another buffer");
-    return MUON_OK;
-  };
-  const muon_status_t st = check();
-  if (st != MUON_OK) { muon::handle_error(h, "%s", why.text); return st; }
-  if (r->batch * r->tokens == 0) return MUON_OK;
-  if (!muon::extents_on_device(h, ext, ne)) return MUON_ERR_INVALID_ARGUMENT;
+constexpr size_t kRotaryBuffers = 2 * muon::kRotaryMax + 2;
+muon_status_t check_rotary(const muon_rotary_t* r, const muon_rotary_tensor_t* t, muon::RotaryArgs& k, Extent* ext,
+                           size_t& ne, Why& why) {
+  Strided bufs[kRotaryBuffers];
+  size_t nb = 0;
+  if (!r || !t) return why.invalid("the request is NULL");
+  if (!known_dtype(r->dtype)) return why.invalid("unknown dtype");
+  if (r->n_tensors < 1 || r->n_tensors > muon::kRotaryMax) return why.invalid("1 to %d tensors a call", muon::kRotaryMax);
+  if (r->head_dim < 1) return why.invalid("head_dim must be >= 1");
+  if (r->head_dim > kMaxRotaryDim) return why.fail(MUON_ERR_UNSUPPORTED, "head_dim %d: at most %d", r->head_dim, kMaxRotaryDim);
+  if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > r->head_dim)
+    return why.invalid("rotary_dim must be even, 2 to head_dim");
+  if (r->layout != 0 && r->layout != 1) return why.invalid("layout must be 0 (halves) or 1 (neighbours)");
+  if (r->inverse != 0 && r->inverse != 1) return why.invalid("inverse must be 0 or 1");
+  if (!std::isfinite(r->scale)) return why.invalid("scale must be finite");
+  if (r->batch < 0 || r->tokens < 0 || r->batch > kMaxTokens || r->tokens > kMaxTokens)
+    return why.invalid("batch or tokens out of range");
+  if (double(r->batch) * double(r->tokens) >= double(1 << 24))  // a token a workgroup at the least
+    return why.fail(MUON_ERR_UNSUPPORTED, "too many tokens in one call (at most 2^24)");
+  const int64_t es = elem_size(r->dtype), all = r->batch * r->tokens;
+  if (all == 0) return MUON_OK;
+  if (!r->freqs) return why.invalid("freqs is NULL");
+  if (reinterpret_cast<uintptr_t>(r->freqs) % 8) return why.invalid("freqs is not 8-byte aligned");
+  bufs[nb++] = flat(r->freqs, r->rotary_dim * 4, false);
+  ext[ne++] = extent(r->freqs, r->rotary_dim * 4);
+  if (r->positions) {
+    const int64_t ps = r->positions_int64 ? 8 : 4;
+    if (reinterpret_cast<uintptr_t>(r->positions) % uintptr_t(ps)) return why.invalid("positions are not aligned to their size");
+    const int64_t bs = r->batch > 1 ? r->position_batch_stride : 0, ts = r->tokens > 1 ? r->position_token_stride : 0;
+    if (bs < 0 || ts < 0 || bs > (int64_t(1) << 40) || ts > (int64_t(1) << 24)) return why.invalid("positions: stride out of range");
+    if (bs > 0 && r->batch > (int64_t(1) << 46) / bs) return why.invalid("positions: extent out of range");
+    const int64_t span = ((r->batch - 1) * bs + (r->tokens - 1) * ts + 1) * ps;
+    bufs[nb++] = flat(r->positions, span, false);
+    ext[ne++] = extent(r->positions, span);
+    k.pos_batch = bs;
+    k.pos_token = ts;
+  }
+  const int half = r->rotary_dim / 2, unit = int(16 / es);
+  for (int i = 0; i < r->n_tensors; ++i) {
+    View x, y;
+    if (t[i].heads < 0 || t[i].heads > 65536) return why.invalid("tensor %d: heads out of range", i);
+    if (t[i].heads == 0) continue;
+    const bool same = t[i].x.data == t[i].y.data;
+    if (same && (t[i].x.batch_stride != t[i].y.batch_stride || t[i].x.token_stride != t[i].y.token_stride ||
+                 t[i].x.head_stride != t[i].y.head_stride))
+      return why.invalid("tensor %d: in place, x and y must have the same strides", i);
+    muon_status_t st = make_view(t[i].x, "x", r->batch, r->tokens, t[i].heads, r->head_dim, es, es, same, x, why);
+    if (st != MUON_OK) return st;
+    if ((st = make_view(t[i].y, "y", r->batch, r->tokens, t[i].heads, r->head_dim, es, es, true, y, why)) != MUON_OK) return st;
+    const auto by16 = [](const Heads& v) {
+      return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.batch % 16 == 0 && v.token % 16 == 0 && v.head % 16 == 0;
+    };
+    k.t[i].x = x.h;
+    k.t[i].y = y.h;
+    k.t[i].heads = int32_t(t[i].heads);
+    k.t[i].vec = by16(x.h) && by16(y.h) && r->head_dim % unit == 0 &&
+                 (r->layout == 1 ? r->rotary_dim : half) % unit == 0;
+    if (!same) { bufs[nb++] = x.s; ext[ne++] = x.e; }
+    bufs[nb++] = y.s;
+    ext[ne++] = y.e;
+  }
+  if (!muon::buffers_disjoint(bufs, nb)) return why.invalid("an output overlaps another buffer");
   k.n = r->n_tensors;
   k.batch = r->batch;
   k.tokens = r->tokens;
@@ -390,6 +381,19 @@ muon_status_t rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_
   k.interleaved = r->layout;
   k.scale = r->scale;
   k.sign = r->inverse ? -1.f : 1.f;
+  return MUON_OK;
+}
+
+muon_status_t rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_tensor_t* t, void* stream) {
+  muon::handle_clear_error(h);
+  Why why;
+  muon::RotaryArgs k{};
+  Extent ext[kRotaryBuffers];
+  size_t ne = 0;
+  const muon_status_t st = check_rotary(r, t, k, ext, ne, why);
+  if (st != MUON_OK) { muon::handle_error(h, "%s", why.text); return st; }
+  if (r->batch * r->tokens == 0) return MUON_OK;
+  if (!muon::extents_on_device(h, ext, ne)) return MUON_ERR_INVALID_ARGUMENT;
   CurrentDevice dev(muon::handle_device(h));
   if (!dev.ok) { muon::handle_error(h, "cannot select device %d", muon::handle_device(h)); return MUON_ERR_DEVICE; }
   const hipError_t e = muon::run_rotary(k, r->dtype == MUON_BF16 ? muon::DT_BF16 : muon::DT_F32,
@@ -399,48 +403,48 @@ muon_status_t rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_
   return MUON_ERR_DEVICE;
 }
 
+muon_status_t check_clip(const muon_qk_clip_t* entries, int64_t n, std::vector<Extent>& ext, Why& why) {
+  std::vector<Strided> bufs;
+  if (n < 0) return why.invalid("n must be >= 0");
+  if (n > 0 && !entries) return why.invalid("entries is NULL");
+  for (int64_t i = 0; i < n; ++i) {
+    const muon_qk_clip_t& e = entries[i];
+    const long long at = (long long)i;
+    if (!known_dtype(e.dtype)) return why.invalid("entry %lld: unknown dtype", at);
+    if (e.reserved != 0) return why.invalid("entry %lld: reserved must be 0", at);
+    if (e.q_heads < 1 || e.kv_heads < 1 || e.q_heads > 65536 || e.q_heads % e.kv_heads)
+      return why.invalid("entry %lld: q_heads must be a positive multiple of kv_heads", at);
+    if (e.head_dim < 1 || e.head_dim > 8192 || e.cols < 1 || e.cols > (int64_t(1) << 28))
+      return why.invalid("entry %lld: head_dim or cols out of range", at);
+    if ((int64_t(e.q_heads) + e.kv_heads) * e.head_dim > kMaxClipRows)
+      return why.fail(MUON_ERR_UNSUPPORTED, "entry %lld: too many rows", at);
+    if (!std::isfinite(e.threshold) || !(e.threshold > 0.f))
+      return why.invalid("entry %lld: threshold must be finite and > 0", at);
+    const int64_t es = elem_size(e.dtype), ql = e.q_ld ? e.q_ld : e.cols, kl = e.k_ld ? e.k_ld : e.cols;
+    if (ql < e.cols || kl < e.cols || ql > (int64_t(1) << 32) || kl > (int64_t(1) << 32))
+      return why.invalid("entry %lld: a row stride must be 0 or at least cols", at);
+    if (!e.wq || !e.wk || !e.max_logits) return why.invalid("entry %lld: NULL pointer", at);
+    const uintptr_t q = reinterpret_cast<uintptr_t>(e.wq), kp = reinterpret_cast<uintptr_t>(e.wk),
+                    m = reinterpret_cast<uintptr_t>(e.max_logits);
+    if (q % uintptr_t(es) || kp % uintptr_t(es) || m % 4)
+      return why.invalid("entry %lld: pointer not aligned to its element size", at);
+    const int64_t rq = int64_t(e.q_heads) * e.head_dim, rk = int64_t(e.kv_heads) * e.head_dim;
+    bufs.push_back(Strided{q, e.cols * es, {ql * es, 0, 0}, {rq, 1, 1}, true});
+    bufs.push_back(Strided{kp, e.cols * es, {kl * es, 0, 0}, {rk, 1, 1}, true});
+    bufs.push_back(flat(e.max_logits, e.q_heads * 4, false));
+    ext.push_back(extent(e.wq, ((rq - 1) * ql + e.cols) * es));
+    ext.push_back(extent(e.wk, ((rk - 1) * kl + e.cols) * es));
+    ext.push_back(extent(e.max_logits, e.q_heads * 4));
+  }
+  if (!muon::buffers_disjoint(bufs.data(), bufs.size())) return why.invalid("weights overlap another buffer");
+  return MUON_OK;
+}
+
 muon_status_t qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n, int reset, void* stream) {
   muon::handle_clear_error(h);
   Why why;
-  std::vector<Strided> bufs;
   std::vector<Extent> ext;
-  const auto check = [&]() -> muon_status_t {
-    if (n < 0) return why.invalid("n must be >= 0");
-    if (n > 0 && !entries) return why.invalid("entries is NULL");
-    if (reset != 0 && reset != 1) return why.invalid("reset must be 0 or 1");
-    for (int64_t i = 0; i < n; ++i) {
-      const muon_qk_clip_t& e = entries[i];
-      const long long at = (long long)i;
-      if (!known_dtype(e.dtype)) return why.invalid("entry %lld: unknown dtype", at);
-      if (e.reserved != 0) return why.invalid("entry %lld: reserved must be 0", at);
-      if (e.q_heads < 1 || e.kv_heads < 1 || e.q_heads > 65536 || e.q_heads % e.kv_heads)
-        return why.invalid("entry %lld: q_heads must be a positive multiple of kv_heads", at);
-      if (e.head_dim < 1 || e.head_dim > 8192 || e.cols < 1 || e.cols > (int64_t(1) << 28))
-        return why.invalid("entry %lld: head_dim or cols out of range", at);
-      if ((int64_t(e.q_heads) + e.kv_heads) * e.head_dim > kMaxClipRows)
-        return why.fail(MUON_ERR_UNSUPPORTED, "entry %lld: too many rows", at);
-      if (!std::isfinite(e.threshold) || !(e.threshold > 0.f))
-        return why.invalid("entry %lld: threshold must be finite and > 0", at);
-      const int64_t es = elem_size(e.dtype), ql = e.q_ld ? e.q_ld : e.cols, kl = e.k_ld ? e.k_ld : e.cols;
-      if (ql < e.cols || kl < e.cols || ql > (int64_t(1) << 32) || kl > (int64_t(1) << 32))
-        return why.invalid("entry %lld: a row stride must be 0 or at least cols", at);
-      if (!e.wq || !e.wk || !e.max_logits) return why.invalid("entry %lld: NULL pointer", at);
-      const uintptr_t q = reinterpret_cast<uintptr_t>(e.wq), kp = reinterpret_cast<uintptr_t>(e.wk),
-                      m = reinterpret_cast<uintptr_t>(e.max_logits);
-      if (q % uintptr_t(es) || kp % uintptr_t(es) || m % 4)
-        return why.invalid("entry %lld: pointer not aligned to its element size", at);
-      const int64_t rq = int64_t(e.q_heads) * e.head_dim, rk = int64_t(e.kv_heads) * e.head_dim;
-      bufs.push_back(Strided{q, e.cols * es, {ql * es, 0, 0}, {rq, 1, 1}, true});
-      bufs.push_back(Strided{kp, e.cols * es, {kl * es, 0, 0}, {rk, 1, 1}, true});
-      bufs.push_back(flat(e.max_logits, e.q_heads * 4, false));
-      ext.push_back(extent(e.wq, ((rq - 1) * ql + e.cols) * es));
-      ext.push_back(extent(e.wk, ((rk - 1) * kl + e.cols) * es));
-      ext.push_back(extent(e.max_logits, e.q_heads * 4));
-    }
-    if (!muon::buffers_disjoint(bufs.data(), bufs.size())) return why.invalid("weights overlap another buffer");
-    return MUON_OK;
-  };
-  const muon_status_t st = check();
+  const muon_status_t st = reset != 0 && reset != 1 ? why.invalid("reset must be 0 or 1") : check_clip(entries, n, ext, why);
   if (st != MUON_OK) { muon::handle_error(h, "%s", why.text); return st; }
   if (n == 0) return MUON_OK;
   if (!muon::extents_on_device(h, ext.data(), ext.size())) return MUON_ERR_INVALID_ARGUMENT;
@@ -506,6 +510,30 @@ muon_status_t muon_validate_attention(const muon_attention_t* a, const muon_atte
     Why why;
     Checked c;
     const muon_status_t st = check_attention(a, g, c, why);
+    tell(why, msg, msg_len);
+    return st;
+  });
+}
+
+muon_status_t muon_validate_rotary(const muon_rotary_t* r, const muon_rotary_tensor_t* tensors, char* msg, size_t msg_len) {
+  if (msg && msg_len) msg[0] = '\0';
+  return guarded(nullptr, [&] {
+    Why why;
+    muon::RotaryArgs k{};
+    Extent ext[kRotaryBuffers];
+    size_t ne = 0;
+    const muon_status_t st = check_rotary(r, tensors, k, ext, ne, why);
+    tell(why, msg, msg_len);
+    return st;
+  });
+}
+
+muon_status_t muon_validate_qk_clip(const muon_qk_clip_t* entries, int64_t n, char* msg, size_t msg_len) {
+  if (msg && msg_len) msg[0] = '\0';
+  return guarded(nullptr, [&] {
+    Why why;
+    std::vector<Extent> ext;
+    const muon_status_t st = check_clip(entries, n, ext, why);
     tell(why, msg, msg_len);
     return st;
   });

@@ -15,7 +15,7 @@ from __future__ import annotations
 
 import torch
 
-from .binding import Muon
+from .binding import Muon, validate_qk_clip
 
 
 def _is_matrix(p: torch.Tensor, group) -> bool:
@@ -27,7 +27,9 @@ def _is_matrix(p: torch.Tensor, group) -> bool:
 
 class MuonAdamW(torch.optim.Optimizer):
     """Muon (momentum, Newton-Schulz orthogonalisation, RMS-matched scale,
-    decoupled decay) for matrix parameters, AdamW for the others.
+    decoupled decay) for matrix parameters, AdamW for the others, and where
+    asked for (`clip_query_keys`) the clip of query and key weights by their
+    attention logits after both.
 
     Per group: `lr`, `momentum` (beta), `nesterov`, `weight_decay`,
     `ns_steps`, `ns_coeffs` (a K x 3 table or None for the constant quintic),
@@ -51,6 +53,27 @@ class MuonAdamW(torch.optim.Optimizer):
             raise ValueError("MuonAdamW needs every parameter on one GPU")
         self._device = next(iter(devices)).index or 0
         self._lib = Muon(self._device)
+        self._clips = []
+
+    def clip_query_keys(self, wq, wk, max_logits, threshold=100.0):
+        """QK-clip (a post-processing stage of Sec. 6.2): from now on every
+        `step()` ends by scaling the rows of the query weight wq [Hq * hd, cols]
+        and the key weight wk [Hkv * hd, cols] of those heads whose largest
+        attention logit exceeds `threshold`, so that it comes down to it, and
+        sets max_logits (fp32, [Hq]) to -inf for the next step's forward passes
+        to raise (`attention(..., max_logits=...)`).  Views of packed weights
+        are fine.  Nothing is read back to the host.  Not part of the state
+        dict: register after loading too."""
+        for t in (wq, wk, max_logits):
+            if t.device.type != "cuda" or (t.device.index or 0) != self._device:
+                raise ValueError("clip_query_keys needs tensors on the parameters' GPU")
+        entry = (wq, wk, max_logits, float(threshold))
+        params = {p.untyped_storage().data_ptr() for g in self.param_groups for p in g["params"]}
+        if any(w.untyped_storage().data_ptr() not in params for w in entry[:2]):
+            raise ValueError("wq and wk must be parameters of this optimizer, or views of them")
+        # (with the earlier ones: no weight is clipped twice)
+        validate_qk_clip(*zip(*[c[:3] for c in self._clips + [entry]]), entry[3])
+        self._clips.append(entry)
 
     def load_state_dict(self, state_dict):
         """As torch's, except that the moments stay fp32: torch casts floating
@@ -118,4 +141,7 @@ class MuonAdamW(torch.optim.Optimizer):
                                      [ms[i] for i in idx], [vs[i] for i in idx], t,
                                      lr=group["adamw_lr"], betas=tuple(group["adamw_betas"]),
                                      eps=group["adamw_eps"], weight_decay=group["adamw_weight_decay"])
+        for threshold in dict.fromkeys(c[3] for c in self._clips):  # one call per threshold
+            wqs, wks, logits, _ = zip(*(c for c in self._clips if c[3] == threshold))
+            self._lib.qk_clip(wqs, wks, logits, threshold, reset=True)
         return loss
