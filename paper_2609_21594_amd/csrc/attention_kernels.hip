@@ -29,6 +29,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kSlack = 6.f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -59,36 +60,81 @@ __device__ __forceinline__ void atomic_max_f32(float* p, float x) {
   else atomicMin(reinterpret_cast<unsigned*>(p), __float_as_uint(x));
 }
 
-template <typename T, int DP>
+// Raises the wave's claim on the SIMD around a row of MFMAs, so that of two
+// waves on a SIMD one runs its products while the other has its softmax,
+// instead of both wanting the same unit.
+template <int P>
+__device__ __forceinline__ void wave_priority() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_setprio(P);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles of heads of up to DU elements, in rows of DP (a power of two).
+template <typename T, int DU>
 struct Lay {
+  static constexpr int DP = DU <= 64 ? 64 : 128;
   static constexpr int ES = sizeof(T), EPC = 16 / ES, CH = DP / EPC, RB = DP * ES;
-  static constexpr int STEPS = CH / 2;   // MFMA steps over the head: 2 chunks each, one per half of the wave
-  static constexpr int DB = DP / 32;     // 32-row blocks of the head
-  __device__ __forceinline__ static int key(int r) {
+  static constexpr int STEPS = DU / EPC / 2;  // MFMA steps over the head: 2 chunks each, one per half of the wave
+  static constexpr int DB = DU / 32;          // 32-row blocks of the head
+  __device__ __forceinline__ static constexpr int key(int r) {
     if constexpr (CH == 8) return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3);
     else return ((r & 3) << 2) | ((r >> 2) & 3);
   }
   __device__ __forceinline__ static int at(int r, int c) { return r * RB + ((c ^ key(r)) << 4); }
 };
 
-__device__ __forceinline__ u32x4_t lds16(const char* p) { return *reinterpret_cast<const u32x4_t*>(p); }
-
-// Stages ROWS rows of `dch` chunks (base: row 0, stride in bytes) into LDS by
-// direct loads of the whole workgroup of 256.  Rows from `left` on repeat the
-// last one and chunks from dch on the last one: what they hold is finite where
-// the operand is, and meets zeros or is never read.
-template <typename T, int DP, int ROWS>
-__device__ __forceinline__ void stage_rows(const char* base, uint32_t stride, int left, int dch, uint32_t lds) {
-  using L = Lay<T, DP>;
-  static_assert(ROWS * L::CH % 256 == 0, "whole loads");
-  const int wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < ROWS * L::CH / 256; ++i) {
-    const int p = i * 256 + threadIdx.x, r = p / L::CH;
-    const int c = min((p % L::CH) ^ L::key(r), dch - 1);
-    load_lds16(base, static_cast<uint32_t>(min(r, left - 1)) * stride + c * 16, lds + (i * 256 + wave * 64) * 16);
-  }
+// LDS by byte address.
+typedef const __attribute__((address_space(3))) u32x4_t* lds_u32x4_p;
+typedef const __attribute__((address_space(3))) uint32_t* lds_u32_p;
+__device__ __forceinline__ u32x4_t lds16(uint32_t at) { return *reinterpret_cast<lds_u32x4_p>(at); }
+__device__ __forceinline__ uint32_t lds4(uint32_t at) { return *reinterpret_cast<lds_u32_p>(at); }
+__device__ __forceinline__ uint2 lds_tr8(uint32_t at) {
+  typedef short v4i16 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) v4i16*>(at)));
 }
+
+// Stages ROWS rows of `dch` chunks into LDS by direct loads of the whole
+// workgroup of 256.  Rows beyond the sequence repeat its last one and chunks
+// from dch on the last one: what they hold is finite where the operand is, and
+// meets zeros or is never read.  Load i of a thread has the row of load 0 plus
+// i * STEP; where 16 divides STEP (or 2 STEP) its chunk, and so its 32-bit
+// offset, is that of load 0 (or of load i % 2) plus a scalar.
+template <typename T, int DP, int ROWS>
+struct Stager {
+  using L = Lay<T, DP>;
+  static constexpr int STEP = 256 / L::CH, N = ROWS * L::CH / 256, NOFF = STEP % 16 == 0 ? 1 : 2;
+  static_assert(ROWS * L::CH % 256 == 0 && NOFF * STEP % 16 == 0 && (N % NOFF == 0), "whole loads");
+  uint32_t off[NOFF];
+  uint32_t stride;
+  __device__ __forceinline__ void init(uint32_t stride_, int dch) {
+    stride = stride_;
+#pragma unroll
+    for (int i = 0; i < NOFF; ++i) {
+      const int r = threadIdx.x / L::CH + i * STEP;
+      off[i] = r * stride + chunk(r, dch) * 16;
+    }
+  }
+  __device__ __forceinline__ static int chunk(int r, int dch) {
+    return min((static_cast<int>(threadIdx.x) % L::CH) ^ L::key(r), dch - 1);
+  }
+  // base: row 0 of the tile; left: rows from there to the sequence's end.
+  __device__ __forceinline__ void issue(const char* base, int left, int dch, uint32_t lds, int wave) const {
+    if (left >= ROWS) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        load_lds16(base + static_cast<int64_t>(i / NOFF * NOFF * STEP) * stride, off[i % NOFF], lds + (i * 256 + wave * 64) * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = threadIdx.x / L::CH + i * STEP;
+        load_lds16(base, static_cast<uint32_t>(min(r, left - 1)) * stride + chunk(r, dch) * 16,
+                   lds + (i * 256 + wave * 64) * 16);
+      }
+    }
+  }
+};
 
 // The lane's row of an operand kept in registers: chunks 2 s + half, zeros
 // beyond the head.
@@ -102,29 +148,48 @@ __device__ __forceinline__ void load_operand(const char* row, int dch, int half,
   }
 }
 
-// A operand of the contraction over the head: rows r0 + lane % 32 of a tile.
+// A operand of the contraction over the head: rows r0 + lane % 32 of a tile,
+// chunks 2 st + half.  As 2 st has no bit in common with half, the swizzled
+// address is a lane's base with bits flipped by a constant, plus a constant:
+// `base` is rows_base + the tile's address (a multiple of 1024, so that the
+// flipped bits are the lane's own), `off` the rest.
 template <typename T, int DP>
-__device__ __forceinline__ u32x4_t frag_rows(const char* tile, int r0, int s, int lane) {
-  return lds16(tile + Lay<T, DP>::at(r0 + (lane & 31), 2 * s + (lane >> 5)));
+__device__ __forceinline__ uint32_t rows_base(int lane) {
+  return Lay<T, DP>::at(lane & 31, lane >> 5);
+}
+template <typename T, int DP>
+__device__ __forceinline__ u32x4_t frag_rows(uint32_t base, int off, int st) {
+  return lds16((base ^ (st << 5)) + off);
 }
 // Steps of a contraction over 32 tile rows: 16 rows each (bf16), 8 (fp32).
 template <typename T> constexpr int kRowSteps = sizeof(T) == 2 ? 2 : 4;
 // A operand of the contraction over tile rows: elements 32 db + lane % 32 of
-// the rows that step `st` of accumulator block rows r0 .. r0 + 31 holds.
+// the rows that step `st` of accumulator block rows r0 .. r0 + 31 holds (r0 a
+// multiple of 32, in `off`).  Rows further by 4, 8 or 16 flip key bits in the
+// same way.
 template <typename T, int DP>
-__device__ __forceinline__ u32x4_t frag_cols(const char* tile, int r0, int st, int db, int lane) {
+__device__ __forceinline__ uint32_t cols_base(int lane) {
   using L = Lay<T, DP>;
   if constexpr (sizeof(T) == 2) {
     const int G = lane >> 4, q = lane & 15;
-    const int r = r0 + 16 * st + 4 * (G >> 1) + (q >> 2), c = 4 * db + 2 * (G & 1) + ((q & 3) >> 1);
-    const uint2 lo = tr_read_b64(tile + L::at(r, c) + (q & 1) * 8), hi = tr_read_b64(tile + L::at(r + 8, c) + (q & 1) * 8);
+    return L::at(4 * (G >> 1) + (q >> 2), 2 * (G & 1) + ((q & 3) >> 1)) + (q & 1) * 8;
+  } else {
+    return L::at(4 * (lane >> 5), (lane & 31) >> 2) + (lane & 3) * 4;
+  }
+}
+template <typename T, int DP>
+__device__ __forceinline__ u32x4_t frag_cols(uint32_t base, int off, int st, int db) {
+  using L = Lay<T, DP>;
+  if constexpr (sizeof(T) == 2) {
+    constexpr int flip = L::key(8) << 4;
+    const uint32_t b = base ^ (db << 6);
+    const uint2 lo = lds_tr8(b + (off + 16 * st * L::RB)), hi = lds_tr8((b ^ flip) + (off + (16 * st + 8) * L::RB));
     return u32x4_t{lo.x, lo.y, hi.x, hi.y};
   } else {
     u32x4_t f;
-    const int d = 32 * db + (lane & 31);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      f[i] = *reinterpret_cast<const uint32_t*>(tile + L::at(r0 + 8 * st + 4 * (lane >> 5) + i, d >> 2) + (d & 3) * 4);
+      f[i] = lds4((base ^ ((db << 7) ^ (L::key(8 * (st & 1) + i) << 4))) + (off + (8 * st + i) * L::RB));
     return f;
   }
 }
@@ -302,14 +367,14 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 }
 
 // ---------------------------------------------------------------------------
-// Forward.  A workgroup of 4 waves holds 128 queries (32 a wave) and passes
-// over the keys in tiles of BN, double-buffered in LDS, keeping the running
-// maximum and sum.
+// Forward.  A workgroup of 4 waves holds 128 NQ queries (32 NQ a wave) and
+// passes over the keys in tiles of BN, double-buffered in LDS, keeping the
+// running maximum and sum.
 // ---------------------------------------------------------------------------
-template <typename T, int DP, int BN, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
+template <typename T, int DP, int NQ, int BN, bool SPLIT>
+__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
   using L = Lay<T, DP>;
-  constexpr int KB = BN / 32, STAGE = 2 * BN * L::RB;
+  constexpr int BM = 128 * NQ, KB = BN / 32, TILE = BN * L::RB, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -321,33 +386,36 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a, int tiles, int 
     bid -= split * items;
   }
   const Item it = item_of(bid, a, pack ? 1 : a.group, tiles, a.causal);
-  const Seq s = find_seq(a.seqs, it.b, it.tile, 128, false);
+  const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
 
-  // the lane's row.  pack: the rows are all heads of the group, each with all queries
+  // the lane's rows.  pack: the rows are all heads of the group, each with all queries
   const int rows = pack ? s.q_rows * a.group : s.q_rows;
-  const int r0 = s.tile * 128 + wave * 32;
-  const bool in = r0 + (lane & 31) < rows;
-  int iq = min(r0 + (lane & 31), rows - 1), g = it.g;
-  if (pack) {
-    g = iq / s.q_rows;
-    iq -= g * s.q_rows;
+  const int r0 = s.tile * BM + wave * 32 * NQ;
+  u32x4_t qf[NQ][L::STEPS];
+  int iq[NQ], head[NQ], jmin[NQ], jmax[NQ];
+  bool in[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = r0 + 32 * n + (lane & 31);
+    in[n] = r < rows;
+    iq[n] = min(r, rows - 1);
+    int g = it.g;
+    if (pack) {
+      g = iq[n] / s.q_rows;
+      iq[n] -= g * s.q_rows;
+    }
+    head[n] = it.kvh * a.group + g;
+    jmax[n] = a.causal ? min(s.nk - 1, iq[n] + shift) : s.nk - 1;
+    jmin[n] = a.causal && a.window ? max(0, iq[n] + shift - a.window + 1) : 0;
+    load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq[n], head[n]), dch, half, qf[n]);
   }
-  const int head = it.kvh * a.group + g;
-  const bool live = in && iq < s.nq;
-  int jmax = s.nk - 1, jmin = 0;
-  if (a.causal) {
-    jmax = min(jmax, iq + shift);
-    if (a.window) jmin = max(0, iq + shift - a.window + 1);
-  }
-  u32x4_t qf[L::STEPS];
-  load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq, head), dch, half, qf);
 
   // the keys of the workgroup and of the wave
   const int last = min(s.q_rows, s.nq) - 1;
-  const KeyRange wg = pack ? keys_of(a, s, 0, last) : keys_of(a, s, s.tile * 128, min(s.tile * 128 + 127, last));
-  const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 31, last));
+  const KeyRange wg = pack ? keys_of(a, s, 0, last) : keys_of(a, s, s.tile * BM, min(s.tile * BM + BM - 1, last));
+  const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 32 * NQ - 1, last));
   int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
   if constexpr (SPLIT) {
     const int per = (max(t1 - t0, 0) + a.splits - 1) / a.splits;
@@ -356,18 +424,28 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a, int tiles, int 
   }
 
   const uint32_t lds0 = lds_offset(smem);
-  const uint32_t kst = static_cast<uint32_t>(a.k.token), vst = static_cast<uint32_t>(a.v.token);
+  const uint32_t rbase = lds0 + rows_base<T, DP>(lane), cbase = lds0 + cols_base<T, DP>(lane);
+  Stager<T, DP, BN> ks, vs;
+  ks.init(static_cast<uint32_t>(a.k.token), dch);
+  vs.init(static_cast<uint32_t>(a.v.token), dch);
+  const char* const krow = at_row(a.k, it.b, s.k0, it.kvh);
+  const char* const vrow = at_row(a.v, it.b, s.k0, it.kvh);
   auto issue = [&](int t) __attribute__((always_inline)) {
     const uint32_t at = lds0 + (t & 1) * STAGE;
-    const int j = t * BN;
-    stage_rows<T, DP, BN>(at_row(a.k, it.b, s.k0 + j, it.kvh), kst, s.nk - j, dch, at);
-    stage_rows<T, DP, BN>(at_row(a.v, it.b, s.k0 + j, it.kvh), vst, s.nk - j, dch, at + BN * L::RB);
+    const int64_t j = t * BN;
+    ks.issue(krow + j * a.k.token, s.nk - t * BN, dch, at, wave);
+    vs.issue(vrow + j * a.v.token, s.nk - t * BN, dch, at + TILE, wave);
   };
 
-  f32x16_t o[L::DB];
+  f32x16_t o[NQ][L::DB];
+  float m[NQ], l[NQ], top[NQ];
 #pragma unroll
-  for (int db = 0; db < L::DB; ++db) o[db] = zero16();
-  float m = -kInf, l = 0.f, top = -kInf;
+  for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db) o[n][db] = zero16();
+    m[n] = top[n] = -kInf;
+    l[n] = 0.f;
+  }
   if (t0 < t1) issue(t0);
   for (int t = t0; t < t1; ++t) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -375,87 +453,115 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a, int tiles, int 
     if (t + 1 < t1) issue(t + 1);
     const int j0 = t * BN;
     if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
-    const char* ks = smem + (t & 1) * STAGE;
-    const char* vs = ks + BN * L::RB;
-    f32x16_t p[KB];
+    const uint32_t rb = rbase + (t & 1) * STAGE, cb = cbase + (t & 1) * STAGE;
+    f32x16_t p[NQ][KB];
+    wave_priority<1>();
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) p[kb] = zero16();
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) p[n][kb] = zero16();
 #pragma unroll
     for (int st = 0; st < L::STEPS; ++st)
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) Mma<T>::run(frag_rows<T, DP>(ks, 32 * kb, st, lane), qf[st], p[kb]);
-    if (j0 + BN > wv.all_end || j0 < wv.all_beg) {
-      const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
+      for (int kb = 0; kb < KB; ++kb) {
+        const u32x4_t kf = frag_rows<T, DP>(rb, 32 * kb * L::RB, st);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) Mma<T>::run(kf, qf[n][st], p[n][kb]);
+      }
+    wave_priority<0>();
+    const bool cut = j0 + BN > wv.all_end || j0 < wv.all_beg;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      if (cut) {
+        asm volatile("; a tile that the mask cuts");  // (a branch: else every tile pays for the comparisons)
+        const int lo = jmin[n] - j0 - 4 * half, hi = jmax[n] - j0 - 4 * half;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+            if (j < lo || j > hi) p[n][kb][r] = -kInf;
+          }
+      }
+      float mx = -kInf;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[n][kb][r]);
+      mx = max32(mx);
+      top[n] = fmaxf(top[n], mx);
+      // Probabilities are taken relative to m, which follows the maximum only
+      // when that has grown by 2^kSlack: binary32 sums have room for the
+      // factor, bf16 rounds relatively, and most tiles leave o as it is.  (The
+      // parts of a split key axis report m as their maximum.)
+      const float mn = mx * a.scale2;
+      if (__any(mn > m[n] + (SPLIT ? 0.f : kSlack))) {
+        const float up = fmaxf(m[n], mn), alpha = m[n] == up ? 1.f : exp2_(m[n] - up);
+        m[n] = up;
+        l[n] *= alpha;
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[n][db][r] *= alpha;
+      }
+      const float mu = m[n] == -kInf ? 0.f : m[n];
+      float sum = 0.f;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
-          if (j < lo || j > hi) p[kb][r] = -kInf;
+          p[n][kb][r] = exp2_(fmaf(p[n][kb][r], a.scale2, -mu));
+          sum += p[n][kb][r];
         }
+      l[n] += sum;
     }
-    float mx = -kInf;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[kb][r]);
-    mx = max32(mx);
-    top = fmaxf(top, mx);
-    const float mn = fmaxf(m, mx * a.scale2);
-    const float mu = mn == -kInf ? 0.f : mn;
-    const float alpha = exp2_(m - mu);
-    m = mn;
-    float sum = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[kb][r] = exp2_(fmaf(p[kb][r], a.scale2, -mu));
-        sum += p[kb][r];
-      }
-    l = fmaf(l, alpha, sum);
-    if (__any(alpha != 1.f)) {
-#pragma unroll
-      for (int db = 0; db < L::DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-    }
+    wave_priority<1>();
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int st = 0; st < kRowSteps<T>; ++st) {
-        const u32x4_t pf = frag_acc<T>(p[kb], st);
+        u32x4_t pf[NQ];
 #pragma unroll
-        for (int db = 0; db < L::DB; ++db) Mma<T>::run(frag_cols<T, DP>(vs, 32 * kb, st, db, lane), pf, o[db]);
+        for (int n = 0; n < NQ; ++n) pf[n] = frag_acc<T>(p[n][kb], st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) {
+          const u32x4_t vf = frag_cols<T, DP>(cb, TILE + 32 * kb * L::RB, st, db);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) Mma<T>::run(vf, pf[n], o[n][db]);
+        }
       }
+    wave_priority<0>();
   }
-  l = sum32(l);
 
-  if constexpr (SPLIT) {
-    const int64_t row = row_index(a, it.b, head, s.q0 + iq);
-    const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
-    float* po = a.part_o + (split * all + row) * a.dim;
-    store_row<float, L::DB>(o, 1.f, reinterpret_cast<char*>(po), nullptr, a.dim / 4, half, in);
-    if (in && half == 0) a.part_ml[split * all + row] = make_float2(m, l);
-    return;
-  }
-  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
-  if (!live) {
 #pragma unroll
-    for (int db = 0; db < L::DB; ++db) o[db] = zero16();
-  }
-  char* orow = at_row_w(a.out, it.b, s.q0 + iq, head);
-  char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq, head) : nullptr;
-  store_row<T, L::DB>(o, inv, orow, rrow, dch, half, in);
-  if (in && half == 0)
-    a.lse[row_index(a, it.b, head, s.q0 + iq)] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
-  if (a.max_logits) {
-    float t = live ? top * a.scale : -kInf;
-    if (pack) {
-      if (half == 0 && t > -kInf) atomic_max_f32(a.max_logits + head, t);
-    } else {
-      t = wave_max(t);
-      if (lane == 0 && t > -kInf) atomic_max_f32(a.max_logits + head, t);
+  for (int n = 0; n < NQ; ++n) {
+    const float sum = sum32(l[n]);
+    const int64_t row = row_index(a, it.b, head[n], s.q0 + iq[n]);
+    if constexpr (SPLIT) {
+      const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
+      float* po = a.part_o + (split * all + row) * a.dim;
+      store_row<float, L::DB>(o[n], 1.f, reinterpret_cast<char*>(po), nullptr, a.dim / 4, half, in[n]);
+      if (in[n] && half == 0) a.part_ml[split * all + row] = make_float2(m[n], sum);
+      continue;
+    }
+    const bool live = in[n] && iq[n] < s.nq;
+    const float inv = !live || sum == 0.f ? 0.f : 1.f / sum;
+    if (!live) {
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db) o[n][db] = zero16();
+    }
+    char* orow = at_row_w(a.out, it.b, s.q0 + iq[n], head[n]);
+    char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq[n], head[n]) : nullptr;
+    store_row<T, L::DB>(o[n], inv, orow, rrow, dch, half, in[n]);
+    if (in[n] && half == 0) a.lse[row] = live && sum != 0.f ? (m[n] + __log2f(sum)) * kLn2 : -kInf;
+    if (a.max_logits) {
+      float x = live ? top[n] * a.scale : -kInf;
+      if (pack) {
+        if (half == 0 && x > -kInf) atomic_max_f32(a.max_logits + head[n], x);
+      } else {
+        x = wave_max(x);
+        if (lane == 0 && x > -kInf) atomic_max_f32(a.max_logits + head[n], x);
+      }
     }
   }
 }
@@ -506,54 +612,16 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // ---------------------------------------------------------------------------
 // Backward.
 // ---------------------------------------------------------------------------
-// Per row: log2 of the sum of exponentials, +inf where no key is visible (so
-// that every probability recomputed from it is 0), and dout . out in fp32,
-// with what the rounding took from out where the caller kept it.  One row per
-// LPR lanes of 16 bytes.
-template <typename T>
-__global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
-  constexpr int EPC = 16 / sizeof(T), LPR = sizeof(T) == 2 ? 16 : 32;
-  const int sub = threadIdx.x % LPR;
-  const int64_t n = static_cast<int64_t>(a.seqs.batch) * a.seqs.q_tokens * a.q_heads;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
-  if (at >= n) return;
-  const int head = static_cast<int>(at % a.q_heads);
-  const int64_t bt = at / a.q_heads;
-  const int i = static_cast<int>(bt % a.seqs.q_tokens), b = static_cast<int>(bt / a.seqs.q_tokens);
-  float x = 0.f;
-  if (sub < a.dim / EPC) {
-    const u32x4_t o = *reinterpret_cast<const u32x4_t*>(at_row(a.out, b, i, head) + sub * 16);
-    const u32x4_t d = *reinterpret_cast<const u32x4_t*>(at_row(a.dout, b, i, head) + sub * 16);
-    if constexpr (sizeof(T) == 2) {
-      u32x4_t e{0, 0, 0, 0};
-      if (a.res.p) e = *reinterpret_cast<const u32x4_t*>(at_row(a.res, b, i, head) + sub * 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x = fmaf(__uint_as_float(d[k] << 16), __uint_as_float(o[k] << 16) + __uint_as_float(e[k] << 16), x);
-        x = fmaf(__uint_as_float(d[k] & 0xffff0000u),
-                 __uint_as_float(o[k] & 0xffff0000u) + __uint_as_float(e[k] & 0xffff0000u), x);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x = fmaf(__uint_as_float(d[k]), __uint_as_float(o[k]), x);
-    }
-  }
-#pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) x += __shfl_xor(x, o);
-  if (sub == 0) {
-    const int64_t row = row_index(a, b, head, i);
-    const float v = a.lse[row];
-    a.lse2[row] = v == -kInf ? kInf : v * kLog2e;
-    a.delta[row] = x;
-  }
-}
-
 // dQ: a wave holds 32 NQ queries (Q and dO rows in registers), the workgroup
 // passes over the keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
+// First it forms each row's dout . out in fp32, with what the rounding took
+// from out where the caller kept it, and writes it and log2 of the sum of
+// exponentials for k_attn_dkv: +inf where no key is visible, so that every
+// probability recomputed from it is 0.
 template <typename T, int DP, int NQ, int BN>
 __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
   using L = Lay<T, DP>;
-  constexpr int BM = 128 * NQ, STAGE = 2 * BN * L::RB;
+  constexpr int BM = 128 * NQ, TILE = BN * L::RB, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -563,6 +631,25 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
   if (!s.ok) return;
   const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
   const int r0 = s.tile * BM + wave * 32 * NQ;
+  const int t0q = s.tile * BM;
+  const KeyRange wg = keys_of(a, s, t0q, min(t0q + BM, s.nq) - 1);
+  const KeyRange wv = keys_of(a, s, r0, min(r0 + 32 * NQ, s.nq) - 1);
+  const int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
+
+  const uint32_t lds0 = lds_offset(smem);
+  const uint32_t rbase = lds0 + rows_base<T, DP>(lane), cbase = lds0 + cols_base<T, DP>(lane);
+  Stager<T, DP, BN> ks, vs;
+  ks.init(static_cast<uint32_t>(a.k.token), dch);
+  vs.init(static_cast<uint32_t>(a.v.token), dch);
+  const char* const krow = at_row(a.k, it.b, s.k0, it.kvh);
+  const char* const vrow = at_row(a.v, it.b, s.k0, it.kvh);
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (t & 1) * STAGE;
+    const int64_t j = t * BN;
+    ks.issue(krow + j * a.k.token, s.nk - t * BN, dch, at, wave);
+    vs.issue(vrow + j * a.v.token, s.nk - t * BN, dch, at + TILE, wave);
+  };
+  if (t0 < t1) issue(t0);
 
   u32x4_t qf[NQ][L::STEPS], df[NQ][L::STEPS];
   float lse2[NQ], delta[NQ];
@@ -572,37 +659,59 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
     const int r = r0 + 32 * n + (lane & 31), iq = min(r, s.q_rows - 1);
     load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq, head), dch, half, qf[n]);
     load_operand<T, DP>(at_row(a.dout, it.b, s.q0 + iq, head), dch, half, df[n]);
+    float x = 0.f;
+    {
+      u32x4_t of[L::STEPS];
+      load_operand<T, DP>(at_row(a.out, it.b, s.q0 + iq, head), dch, half, of);
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2) {
+            x = fmaf(__uint_as_float(df[n][st][e] << 16), __uint_as_float(of[st][e] << 16), x);
+            x = fmaf(__uint_as_float(df[n][st][e] & 0xffff0000u), __uint_as_float(of[st][e] & 0xffff0000u), x);
+          } else {
+            x = fmaf(__uint_as_float(df[n][st][e]), __uint_as_float(of[st][e]), x);
+          }
+        }
+    }
+    if constexpr (sizeof(T) == 2) {
+      if (a.res.p) {
+        u32x4_t of[L::STEPS];
+        load_operand<T, DP>(at_row(a.res, it.b, s.q0 + iq, head), dch, half, of);
+        float y = 0.f;
+#pragma unroll
+        for (int st = 0; st < L::STEPS; ++st)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y = fmaf(__uint_as_float(df[n][st][e] << 16), __uint_as_float(of[st][e] << 16), y);
+            y = fmaf(__uint_as_float(df[n][st][e] & 0xffff0000u), __uint_as_float(of[st][e] & 0xffff0000u), y);
+          }
+        x += y;
+      }
+    }
+    x = sum32(x);
     const int64_t row = row_index(a, it.b, head, s.q0 + iq);
-    lse2[n] = r < s.nq ? a.lse2[row] : kInf;
-    delta[n] = a.delta[row];
+    const float v = r < s.nq ? a.lse[row] : -kInf;
+    lse2[n] = v == -kInf ? kInf : v * kLog2e;
+    delta[n] = x;
+    if (half == 0 && r < s.nq) {
+      a.lse2[row] = lse2[n];
+      a.delta[row] = x;
+    }
     jmax[n] = a.causal ? min(s.nk - 1, iq + shift) : s.nk - 1;
     jmin[n] = a.causal && a.window ? max(0, iq + shift - a.window + 1) : 0;
   }
-  const int t0q = s.tile * BM;
-  const KeyRange wg = keys_of(a, s, t0q, min(t0q + BM, s.nq) - 1);
-  const KeyRange wv = keys_of(a, s, r0, min(r0 + 32 * NQ, s.nq) - 1);
-  const int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
-
-  const uint32_t lds0 = lds_offset(smem);
-  const uint32_t kst = static_cast<uint32_t>(a.k.token), vst = static_cast<uint32_t>(a.v.token);
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + (t & 1) * STAGE;
-    const int j = t * BN;
-    stage_rows<T, DP, BN>(at_row(a.k, it.b, s.k0 + j, it.kvh), kst, s.nk - j, dch, at);
-    stage_rows<T, DP, BN>(at_row(a.v, it.b, s.k0 + j, it.kvh), vst, s.nk - j, dch, at + BN * L::RB);
-  };
   f32x16_t acc[NQ][L::DB];
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
 #pragma unroll
     for (int db = 0; db < L::DB; ++db) acc[n][db] = zero16();
-  if (t0 < t1) issue(t0);
   for (int t = t0; t < t1; ++t) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (t + 1 < t1) issue(t + 1);
-    const char* ks = smem + (t & 1) * STAGE;
-    const char* vs = ks + BN * L::RB;
+    const uint32_t rb = rbase + (t & 1) * STAGE, cb = cbase + (t & 1) * STAGE;
 #pragma unroll
     for (int kb = 0; kb < BN / 32; ++kb) {
       const int j0 = t * BN + 32 * kb;
@@ -610,22 +719,25 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
       f32x16_t p[NQ], d[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) p[n] = d[n] = zero16();
+      if constexpr (NQ == 1) wave_priority<1>();
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t kf = frag_rows<T, DP>(ks, 32 * kb, st, lane);
+        const u32x4_t kf = frag_rows<T, DP>(rb, 32 * kb * L::RB, st);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) Mma<T>::run(kf, qf[n][st], p[n]);
       }
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t vf = frag_rows<T, DP>(vs, 32 * kb, st, lane);
+        const u32x4_t vf = frag_rows<T, DP>(rb, TILE + 32 * kb * L::RB, st);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) Mma<T>::run(vf, df[n][st], d[n]);
       }
+      if constexpr (NQ == 1) wave_priority<0>();
       const bool cut = j0 + 32 > wv.all_end || j0 < wv.all_beg;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         if (cut) {
+          asm volatile("; a tile that the mask cuts");
           const int lo = jmin[n] - j0 - 4 * half, hi = jmax[n] - j0 - 4 * half;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -637,6 +749,7 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
         for (int r = 0; r < 16; ++r)
           d[n][r] = exp2_(fmaf(p[n][r], a.scale2, -lse2[n])) * (d[n][r] - delta[n]);
       }
+      if constexpr (NQ == 1) wave_priority<1>();
 #pragma unroll
       for (int st = 0; st < kRowSteps<T>; ++st) {
         u32x4_t f[NQ];
@@ -644,11 +757,12 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
         for (int n = 0; n < NQ; ++n) f[n] = frag_acc<T>(d[n], st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t kt = frag_cols<T, DP>(ks, 32 * kb, st, db, lane);
+          const u32x4_t kt = frag_cols<T, DP>(cb, 32 * kb * L::RB, st, db);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) Mma<T>::run(kt, f[n], acc[n][db]);
         }
       }
+      if constexpr (NQ == 1) wave_priority<0>();
     }
   }
 #pragma unroll
@@ -662,14 +776,15 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
   }
 }
 
-// dK, dV: a wave holds 32 NK keys (K and V rows in registers), the workgroup
-// passes over the queries of one head, or of all heads of the group:
-// S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
-template <typename T, int DP, int NK, int BM>
-__global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
+// dK, dV: a wave holds 32 NK keys (K rows in registers, V rows there or, VL,
+// in LDS), the workgroup passes over the queries of one head, or of all heads
+// of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+template <typename T, int DP, int NK, int BM, bool VL>
+__global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
   using L = Lay<T, DP>;
-  constexpr int BK = 128 * NK, DATA = 2 * BM * L::RB, STAGE = DATA + 2 * BM * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  constexpr int BK = 128 * NK, TILE = BM * L::RB, STAGE = 2 * TILE, VT = VL ? BK * L::RB : 0;
+  // V, two stages of Q and dO, two of the rows' statistics (64 floats of each kind)
+  __shared__ __attribute__((aligned(1024))) char smem[VT + 2 * STAGE + 1024];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int dch = a.dim / L::EPC;
@@ -678,17 +793,6 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
   const int k0 = s.tile * BK, w0 = k0 + wave * 32 * NK;
-
-  u32x4_t kf[NK][L::STEPS], vf[NK][L::STEPS];
-  int qmin[NK], qmax[NK];
-#pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    const int j = min(w0 + 32 * n + (lane & 31), s.k_rows - 1);
-    load_operand<T, DP>(at_row(a.k, it.b, s.k0 + j, it.kvh), dch, half, kf[n]);
-    load_operand<T, DP>(at_row(a.v, it.b, s.k0 + j, it.kvh), dch, half, vf[n]);
-    qmin[n] = a.causal ? j - shift : 0;
-    qmax[n] = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
-  }
   // queries that see a key of the workgroup
   int qb = 0, qe = s.nq;
   if (a.causal) {
@@ -700,36 +804,65 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
   const int heads = a.kv_split ? 1 : a.group, steps = per * heads;
   const int h0 = it.kvh * a.group + (a.kv_split ? it.g : 0);
 
-  const uint32_t lds0 = lds_offset(smem);
-  const uint32_t qst = static_cast<uint32_t>(a.q.token), dst = static_cast<uint32_t>(a.dout.token);
+  const uint32_t lds0 = lds_offset(smem), stats = lds0 + VT + 2 * STAGE;
+  const uint32_t rbase = lds0 + VT + rows_base<T, DP>(lane), cbase = lds0 + VT + cols_base<T, DP>(lane);
+  const uint32_t vbase = lds0 + wave * 32 * NK * L::RB + rows_base<T, DP>(lane);
+  Stager<T, DP, BM> qs, ds;
+  qs.init(static_cast<uint32_t>(a.q.token), dch);
+  ds.init(static_cast<uint32_t>(a.dout.token), dch);
+  const char* const qrow = at_row(a.q, it.b, s.q0, h0);
+  const char* const drow = at_row(a.dout, it.b, s.q0, h0);
+  const int64_t srow = row_index(a, it.b, h0, s.q0);
+  // the next tile to load: tile nt of head h0 + nh
+  int nt = t0, nh = 0;
   auto issue = [&](int i) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + (i & 1) * STAGE;
-    const int head = h0 + i / per, q = (t0 + i % per) * BM, left = s.nq - q;
-    stage_rows<T, DP, BM>(at_row(a.q, it.b, s.q0 + q, head), qst, left, dch, at);
-    stage_rows<T, DP, BM>(at_row(a.dout, it.b, s.q0 + q, head), dst, left, dch, at + BM * L::RB);
-    // the rows' statistics (queries behind the last repeat it, and are masked)
-    if (threadIdx.x < 2 * BM) {
-      const int r = threadIdx.x % BM;
-      const int64_t row = row_index(a, it.b, head, s.q0 + q + min(r, left - 1));
-      const float v = threadIdx.x < BM ? a.lse2[row] : a.delta[row];
-      *reinterpret_cast<float*>(smem + (i & 1) * STAGE + DATA + threadIdx.x * 4) = v;
+    const uint32_t at = lds0 + VT + (i & 1) * STAGE;
+    const int64_t q = nt * BM;
+    const int left = s.nq - nt * BM;
+    qs.issue(qrow + nh * a.q.head + q * a.q.token, left, dch, at, wave);
+    ds.issue(drow + nh * a.dout.head + q * a.dout.token, left, dch, at + TILE, wave);
+    if (wave < 2) {  // the rows' statistics (queries behind the last repeat it, and are masked)
+      const float* p = (wave ? a.delta : a.lse2) + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q;
+      load_lds4(reinterpret_cast<const char*>(p), min(min(lane, BM - 1), left - 1) * 4, stats + (i & 1) * 512 + wave * 256);
     }
+    if (++nt == t0 + per) { nt = t0; ++nh; }
   };
+  if (steps > 0) issue(0);
+
+  u32x4_t kf[NK][L::STEPS], vf[VL ? 1 : NK][VL ? 1 : L::STEPS];
+  int qmin[NK], qmax[NK];
+#pragma unroll
+  for (int n = 0; n < NK; ++n) {
+    const int j = min(w0 + 32 * n + (lane & 31), s.k_rows - 1);
+    load_operand<T, DP>(at_row(a.k, it.b, s.k0 + j, it.kvh), dch, half, kf[n]);
+    if constexpr (!VL) load_operand<T, DP>(at_row(a.v, it.b, s.k0 + j, it.kvh), dch, half, vf[n]);
+    qmin[n] = a.causal ? j - shift : 0;
+    qmax[n] = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
+  }
+  if constexpr (VL) {
+    if (steps > 0)  // zeros beyond the head: dO's tiles repeat a chunk there
+      for (int p = threadIdx.x; p < BK * L::CH; p += 256) {
+        const int r = p / L::CH, c = p % L::CH;
+        const char* row = at_row(a.v, it.b, s.k0 + min(k0 + r, s.nk - 1), it.kvh);
+        *reinterpret_cast<u32x4_t*>(smem + L::at(r, c)) =
+            c < dch ? *reinterpret_cast<const u32x4_t*>(row + c * 16) : u32x4_t{0, 0, 0, 0};
+      }
+  }
   f32x16_t dk[NK][L::DB], dv[NK][L::DB];
 #pragma unroll
   for (int n = 0; n < NK; ++n)
 #pragma unroll
     for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = zero16();
   const int wk_hi = min(w0 + 32 * NK, s.nk) - 1;  // the wave's last key
-  if (steps > 0) issue(0);
+  int ct = t0;
   for (int i = 0; i < steps; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (i + 1 < steps) issue(i + 1);
-    const char* qs = smem + (i & 1) * STAGE;
-    const char* os = qs + BM * L::RB;
-    const char* ss = qs + DATA;
-    const int q0 = (t0 + i % per) * BM;
+    const uint32_t rb = rbase + (i & 1) * STAGE, cb = cbase + (i & 1) * STAGE;
+    const uint32_t sb = stats + (i & 1) * 512 + 16 * half;
+    const int q0 = ct * BM;
+    if (++ct == t0 + per) ct = t0;
 #pragma unroll
     for (int qk = 0; qk < BM / 32; ++qk) {
       const int q = q0 + 32 * qk;
@@ -741,37 +874,48 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
       f32x16_t p[NK], d[NK];
 #pragma unroll
       for (int n = 0; n < NK; ++n) p[n] = d[n] = zero16();
+      if constexpr (NK == 1) wave_priority<1>();
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t f = frag_rows<T, DP>(qs, 32 * qk, st, lane);
+        const u32x4_t f = frag_rows<T, DP>(rb, 32 * qk * L::RB, st);
 #pragma unroll
         for (int n = 0; n < NK; ++n) Mma<T>::run(f, kf[n][st], p[n]);
       }
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t f = frag_rows<T, DP>(os, 32 * qk, st, lane);
+        const u32x4_t f = frag_rows<T, DP>(rb, TILE + 32 * qk * L::RB, st);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) Mma<T>::run(f, vf[n][st], d[n]);
+        for (int n = 0; n < NK; ++n) {
+          if constexpr (VL) Mma<T>::run(f, frag_rows<T, DP>(vbase, 32 * n * L::RB, st), d[n]);
+          else Mma<T>::run(f, vf[n][st], d[n]);
+        }
+      }
+      if constexpr (NK == 1) wave_priority<0>();
+      if (cut) {
+        asm volatile("; a tile that the mask cuts");
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+          const int lo = qmin[n] - q - 4 * half, hi = qmax[n] - q - 4 * half;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int i = 8 * (r >> 2) + (r & 3);
+            if (i < lo || i > hi) p[n][r] = -kInf;
+          }
+        }
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 ls = *reinterpret_cast<const float4*>(ss + (32 * qk + 8 * g + 4 * half) * 4);
-        const float4 de = *reinterpret_cast<const float4*>(ss + (BM + 32 * qk + 8 * g + 4 * half) * 4);
-        const float lv[4] = {ls.x, ls.y, ls.z, ls.w}, dl[4] = {de.x, de.y, de.z, de.w};
+        const u32x4_t ls = lds16(sb + (32 * qk + 8 * g) * 4), de = lds16(sb + 256 + (32 * qk + 8 * g) * 4);
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float x = p[n][4 * g + e];
-            if (cut) {
-              const int qq = q + 8 * g + 4 * half + e;
-              if (qq < qmin[n] || qq > qmax[n]) x = -kInf;
-            }
-            x = exp2_(fmaf(x, a.scale2, -lv[e]));
+            const float x = exp2_(fmaf(p[n][4 * g + e], a.scale2, -__uint_as_float(ls[e])));
             p[n][4 * g + e] = x;
-            d[n][4 * g + e] = x * (d[n][4 * g + e] - dl[e]);
+            d[n][4 * g + e] = x * (d[n][4 * g + e] - __uint_as_float(de[e]));
           }
       }
+      if constexpr (NK == 1) wave_priority<1>();
 #pragma unroll
       for (int st = 0; st < kRowSteps<T>; ++st) {
         u32x4_t f[NK];
@@ -779,7 +923,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
         for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(p[n], st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t x = frag_cols<T, DP>(os, 32 * qk, st, db, lane);
+          const u32x4_t x = frag_cols<T, DP>(cb, TILE + 32 * qk * L::RB, st, db);
 #pragma unroll
           for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dv[n][db]);
         }
@@ -791,11 +935,12 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, int tiles) {
         for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(d[n], st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t x = frag_cols<T, DP>(qs, 32 * qk, st, db, lane);
+          const u32x4_t x = frag_cols<T, DP>(cb, 32 * qk * L::RB, st, db);
 #pragma unroll
           for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dk[n][db]);
         }
       }
+      if constexpr (NK == 1) wave_priority<0>();
     }
   }
 #pragma unroll
@@ -999,14 +1144,14 @@ bool packs_heads(const Seqs& s, int group) {
   return !s.q_off && group > 1 && int64_t(s.q_tokens) * group <= 128;
 }
 
-template <typename T, int DP, int BN>
+template <typename T, int DP, int NQ, int BN>
 hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   const bool pack = packs_heads(a.seqs, a.group);
-  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128);
+  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128 * NQ);
   const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
   const dim3 g(static_cast<unsigned>(grid)), b(256);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
-  else hipLaunchKernelGGL((k_attn_fwd<T, DP, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
+  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, NQ, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
+  else hipLaunchKernelGGL((k_attn_fwd<T, DP, NQ, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
@@ -1014,25 +1159,20 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T, int DP, int NB, int TILE>
+template <typename T, int DP, int NQ, int NK, int TQ, int TK, bool VL>
 hipError_t backward_of(const AttnArgs& a, hipStream_t st) {
-  constexpr int LPR = sizeof(T) == 2 ? 16 : 32;
-  const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
   const dim3 b(256);
   hipError_t e;
-  if (rows > 0) {
-    const int64_t per = 256 / LPR;
-    hipLaunchKernelGGL((k_attn_delta<T>), dim3(static_cast<unsigned>((rows + per - 1) / per)), b, 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 * NB);
-    hipLaunchKernelGGL((k_attn_dq<T, DP, NB, TILE>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
+  if (a.seqs.q_tokens > 0) {
+    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 * NQ);
+    hipLaunchKernelGGL((k_attn_dq<T, DP, NQ, TQ>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
                        st, a, int(tiles));
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.seqs.k_tokens == 0) return hipSuccess;
-  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 * NB);
+  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 * NK);
   const int64_t grid = a.seqs.batch * a.kv_heads * (a.kv_split ? a.group : 1) * tiles;
-  hipLaunchKernelGGL((k_attn_dkv<T, DP, NB, TILE>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
+  hipLaunchKernelGGL((k_attn_dkv<T, DP, NK, TK, VL>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
   if ((e = hipGetLastError()) != hipSuccess || !a.kv_split) return e;
   const int64_t n = 2 * a.seqs.batch * int64_t(a.seqs.k_tokens) * a.kv_heads * (a.dim / 4);
   hipLaunchKernelGGL((k_attn_sum_heads<T>), dim3(static_cast<unsigned>((n + 255) / 256)), b, 0, st, a);
@@ -1059,8 +1199,13 @@ hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, L
   if (a.seqs.batch * a.seqs.q_tokens == 0) return hipSuccess;
   Timed tm(timer, KK_ATTENTION_FWD, st);
   hipError_t e;
-  if (dtype == DT_BF16) e = a.dim <= 64 ? forward_of<uint16_t, 64, 64>(a, st) : forward_of<uint16_t, 128, 64>(a, st);
-  else e = a.dim <= 64 ? forward_of<float, 64, 64>(a, st) : forward_of<float, 128, 32>(a, st);
+  const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
+  if (dtype == DT_BF16)
+    e = pick([&] { return forward_of<uint16_t, 64, 1, 64>(a, st); }, [&] { return forward_of<uint16_t, 96, 1, 64>(a, st); },
+             [&] { return forward_of<uint16_t, 128, 1, 64>(a, st); });
+  else
+    e = pick([&] { return forward_of<float, 64, 1, 64>(a, st); }, [&] { return forward_of<float, 96, 1, 32>(a, st); },
+             [&] { return forward_of<float, 128, 1, 32>(a, st); });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(4.0 * pairs_of(a) * a.dim, 0,
@@ -1072,8 +1217,14 @@ hipError_t run_attention_backward(const AttnArgs& a, int dtype, hipStream_t st, 
   if (a.seqs.batch == 0) return hipSuccess;
   Timed tm(timer, KK_ATTENTION_BWD, st);
   hipError_t e;
-  if (dtype == DT_BF16) e = a.dim <= 64 ? backward_of<uint16_t, 64, 2, 64>(a, st) : backward_of<uint16_t, 128, 2, 64>(a, st);
-  else e = a.dim <= 64 ? backward_of<float, 64, 1, 32>(a, st) : backward_of<float, 128, 1, 32>(a, st);
+  const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
+  if (dtype == DT_BF16)
+    e = pick([&] { return backward_of<uint16_t, 64, 1, 1, 64, 32, false>(a, st); },
+             [&] { return backward_of<uint16_t, 96, 1, 1, 64, 32, true>(a, st); }, [&] { return backward_of<uint16_t, 128, 1, 1, 64, 32, true>(a, st); });
+  else
+    e = pick([&] { return backward_of<float, 64, 1, 1, 32, 32, false>(a, st); },
+             [&] { return backward_of<float, 96, 1, 1, 32, 32, true>(a, st); },
+             [&] { return backward_of<float, 128, 1, 1, 32, 32, true>(a, st); });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(10.0 * pairs_of(a) * a.dim, 0,

@@ -111,6 +111,16 @@ __device__ __forceinline__ void load_lds16(const char* base, uint32_t off, uint3
                :: "v"(off), "s"(bs), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
 }
 
+// The same with 4 bytes a lane (global_load_lds_dword).
+__device__ __forceinline__ void load_lds4(const char* base, uint32_t off, uint32_t lds) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b >> 32)));
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b & 0xffffffffu)));
+  const uint64_t bs = (static_cast<uint64_t>(hi) << 32) | static_cast<uint64_t>(lo);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :: "v"(off), "s"(bs), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+}
+
 // 8 bytes per lane from LDS through the transposing read (ds_read_b64_tr_b16).
 __device__ __forceinline__ uint2 tr_read_b64(const char* p) {
   typedef short v4i16 __attribute__((ext_vector_type(4)));
