@@ -622,17 +622,13 @@ class Muon:
 
     # ---- the attention block of a training step ---------------------------------
 
-    def _on(self, stream):
-        """(stream pointer, context): outputs and scratch are allocated on the
-        stream that the call runs on."""
-        import contextlib
+    def _stream(self):
         import torch
-        if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream, contextlib.nullcontext()
-        return stream.cuda_stream, torch.cuda.stream(stream)
+        return torch.cuda.current_stream(self.device).cuda_stream
 
-    def _scratch(self, record, backward):
-        """(keepalive, pointer, bytes) of the scratch memory a request needs."""
+    def _scratch(self, record, backward, like):
+        """(keepalive, pointer, bytes) of the scratch memory a request needs,
+        of the current stream."""
         import torch
         n = ctypes.c_size_t()
         st = self.lib.muon_attention_scratch(record, backward, ctypes.byref(n))
@@ -642,7 +638,7 @@ class Muon:
             raise MuonError(st, msg.value.decode())
         if n.value == 0:
             return None, 0, 0
-        t = torch.empty(n.value + 256, dtype=torch.uint8, device=torch.device("cuda", self.device))
+        t = like.new_empty(n.value + 256, dtype=torch.uint8)
         return t, (t.data_ptr() + 255) & ~255, n.value
 
     def attention(self, q, k, v, scale=None, causal=False, window=0, q_offsets=None, k_offsets=None, q_lens=None,
@@ -660,6 +656,10 @@ class Muon:
         receives what the rounding took from out, for attention_backward.
         lse is fp32, [B, Hq, Sq] ([Hq, Sq] packed)."""
         import torch
+        if stream is not None:  # results and scratch belong to the stream that the call runs on
+            with torch.cuda.stream(stream):
+                return self.attention(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens, max_logits,
+                                      out, residual)
         a = _Attention(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
         _check_device([t for t in (q, k, v, max_logits, out, residual, *a.lists) if t is not None], self.device)
         if max_logits is not None:
@@ -669,15 +669,16 @@ class Muon:
         for t, what in ((out, "out"), (residual, "residual")):
             if t is not None:
                 _expect(t, q.shape, q.dtype, what)
-        ptr, ctx = self._on(stream)
-        with ctx:
-            keep, at, n = self._scratch(a.sizes(), 0)
-            if out is None:  # rows outside packed sequences are not written
-                out = (torch.empty if q_offsets is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-            lse = (torch.empty(a.lse_shape, dtype=torch.float32, device=q.device) if q_offsets is None else
-                   torch.full(a.lse_shape, -float("inf"), dtype=torch.float32, device=q.device))
-            self._check(self.lib.muon_attention_forward(self.h, a.record(out, residual, lse, max_logits, at, n), ptr))
-            del keep
+        keep, at, n = self._scratch(a.sizes(), 0, q)
+        if q_offsets is None:
+            out = q.new_empty(a.q_shape) if out is None else out
+            lse = q.new_empty(a.lse_shape, dtype=torch.float32)
+        else:  # rows outside packed sequences are not written
+            out = q.new_zeros(a.q_shape) if out is None else out
+            lse = q.new_full(a.lse_shape, -float("inf"), dtype=torch.float32)
+        self._check(self.lib.muon_attention_forward(self.h, a.record(out, residual, lse, max_logits, at, n),
+                                                    self._stream()))
+        del keep
         return out, lse
 
     def attention_backward(self, dout, q, k, v, out, lse, residual=None, scale=None, causal=False, window=0,
@@ -688,6 +689,10 @@ class Muon:
         forward pass had them.  dq, dk, dv may be given (slices of one tensor
         are fine)."""
         import torch
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.attention_backward(dout, q, k, v, out, lse, residual, scale, causal, window, q_offsets,
+                                               k_offsets, q_lens, k_lens, dq, dk, dv)
         a = _Attention(q, k, v, scale, causal, window, q_offsets, k_offsets, q_lens, k_lens)
         _check_device([t for t in (dout, q, k, v, out, lse, residual, dq, dk, dv, *a.lists) if t is not None],
                       self.device)
@@ -698,16 +703,15 @@ class Muon:
         _expect(lse, a.lse_shape, torch.float32, "lse")
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
-        ptr, ctx = self._on(stream)
-        with ctx:
-            keep, at, n = self._scratch(a.sizes(), 1)
-            new = torch.empty if q_offsets is None else torch.zeros
-            dq = new(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-            dk = new(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-            dv = new(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-            grad = _GRAD_PACK.pack(*_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv))
-            self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n), grad, ptr))
-            del keep
+        keep, at, n = self._scratch(a.sizes(), 1, q)
+        new = q.new_empty if q_offsets is None else q.new_zeros
+        dq = new(a.q_shape) if dq is None else dq
+        dk = new(a.k_shape) if dk is None else dk
+        dv = new(a.k_shape) if dv is None else dv
+        grad = _GRAD_PACK.pack(*_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv))
+        self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n), grad,
+                                                     self._stream()))
+        del keep
         return dq, dk, dv
 
     def rotary(self, xs, freqs, positions=None, first=0, layout="half", scale=1.0, inverse=False, outs=None,
@@ -721,6 +725,9 @@ class Muon:
         turns backwards: the gradient's form.  outs: results' tensors; the
         inputs themselves for in place."""
         import torch
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.rotary(xs, freqs, positions, first, layout, scale, inverse, outs)
         one = torch.is_tensor(xs)
         xs = [xs] if one else list(xs)
         if not 1 <= len(xs) <= 4:
@@ -750,19 +757,17 @@ class Muon:
             for t, y in zip(xs, outs):
                 _expect(y, t.shape, t.dtype, "out")
         _check_device([*xs, freqs, *([] if positions is None else [positions]), *(outs or [])], self.device)
-        ptr, ctx = self._on(stream)
-        with ctx:
-            if outs is None:
-                outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
-            batch, tokens = lead if len(lead) == 2 else (1, lead[0])
-            pst = (0, 0) if positions is None else (positions.stride() if len(lead) == 2 else (0, positions.stride(0)))
-            rec = _ROTARY_PACK.pack(_dtype_code(x), d, 2 * freqs.numel(), int(layout == "interleaved"),
-                                    int(bool(inverse)), float(scale), batch, tokens,
-                                    0 if positions is None else positions.data_ptr(), *pst, int(first),
-                                    freqs.data_ptr(), int(positions is not None and positions.dtype == torch.int64),
-                                    len(xs))
-            ts = b"".join(_ROTARY_TENSOR_PACK.pack(*_heads(t), *_heads(y), t.shape[-2]) for t, y in zip(xs, outs))
-            self._check(self.lib.muon_rotary(self.h, rec, ts, ptr))
+        if outs is None:
+            outs = [t.new_empty(t.shape) for t in xs]
+        batch, tokens = lead if len(lead) == 2 else (1, lead[0])
+        pst = (0, 0) if positions is None else (positions.stride() if len(lead) == 2 else (0, positions.stride(0)))
+        rec = _ROTARY_PACK.pack(_dtype_code(x), d, 2 * freqs.numel(), int(layout == "interleaved"),
+                                int(bool(inverse)), float(scale), batch, tokens,
+                                0 if positions is None else positions.data_ptr(), *pst, int(first),
+                                freqs.data_ptr(), int(positions is not None and positions.dtype == torch.int64),
+                                len(xs))
+        ts = b"".join(_ROTARY_TENSOR_PACK.pack(*_heads(t), *_heads(y), t.shape[-2]) for t, y in zip(xs, outs))
+        self._check(self.lib.muon_rotary(self.h, rec, ts, self._stream()))
         return outs[0] if one else outs
 
     def qk_clip(self, wqs, wks, max_logits, threshold, reset=False, stream=None):
@@ -775,9 +780,8 @@ class Muon:
             raise ValueError("query weights, key weights and logits must have equal length")
         _check_device([*wqs, *wks, *max_logits], self.device)
         recs = clip_records(wqs, wks, max_logits, threshold)
-        ptr, ctx = self._on(stream)
-        with ctx:
-            self._check(self.lib.muon_qk_clip(self.h, recs, n, int(bool(reset)), ptr))
+        ptr = self._stream() if stream is None else stream.cuda_stream
+        self._check(self.lib.muon_qk_clip(self.h, recs, n, int(bool(reset)), ptr))
 
 
 def validate_step(entries: Sequence[MuonParam], hp: MuonHParams):

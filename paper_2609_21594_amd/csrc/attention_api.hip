@@ -21,7 +21,7 @@ using muon::Strided;
 
 constexpr int64_t kMaxTokens = int64_t(1) << 30;   // token counts and tile indices are 32 bits on the device
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;  // bytes: a tile's rows are addressed by 32-bit offsets
-constexpr int64_t kMaxClipBlocks = 1 << 23, kMaxClipRows = kMaxClipBlocks * muon::kClipRows;
+constexpr int64_t kMaxClipBlocks = 1 << 23, kMaxClipRows = kMaxClipBlocks * muon::kClipRowsFew;
 constexpr int kMaxHeadDim = 128, kMaxRotaryDim = 1024;
 
 struct Why {
@@ -451,11 +451,15 @@ muon_status_t qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n,
   CurrentDevice dev(muon::handle_device(h));
   if (!dev.ok) { muon::handle_error(h, "cannot select device %d", muon::handle_device(h)); return MUON_ERR_DEVICE; }
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  int64_t all = 0;
+  for (int64_t i = 0; i < n; ++i) all += (int64_t(entries[i].q_heads) + entries[i].kv_heads) * entries[i].head_dim;
+  const int32_t per = all / muon::kClipRows >= 1024 ? muon::kClipRows : muon::kClipRowsFew;
   // every clip is enqueued before any reset: entries may share logits
   for (int pass = 0; pass < (reset ? 2 : 1); ++pass)
     for (int dt : {MUON_BF16, MUON_F32})
       for (int64_t i = 0; i < n;) {
         muon::ClipArgs k{};
+        k.rows = per;
         for (; i < n && k.n < muon::kClipMax; ++i) {
           const muon_qk_clip_t& e = entries[i];
           if (e.dtype != dt) continue;
@@ -474,7 +478,7 @@ muon_status_t qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n,
           c.vec = reinterpret_cast<uintptr_t>(e.wq) % 16 == 0 && reinterpret_cast<uintptr_t>(e.wk) % 16 == 0 &&
                   c.ldq % 16 == 0 && c.ldk % 16 == 0;
           const int64_t rows = (int64_t(e.q_heads) + e.kv_heads) * e.head_dim;
-          const int64_t blocks = (rows + muon::kClipRows - 1) / muon::kClipRows;
+          const int64_t blocks = (rows + per - 1) / per;
           if (k.first[k.n] + blocks > 2 * kMaxClipBlocks - 1) break;  // the next launch takes it
           k.first[k.n + 1] = int32_t(k.first[k.n] + blocks);
           ++k.n;

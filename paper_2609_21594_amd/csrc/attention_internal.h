@@ -90,10 +90,14 @@ struct ClipArgs {
   ClipEntry e[kClipMax];
   int32_t first[kClipMax + 1];  // first workgroup of each entry
   int32_t n;
+  int32_t rows;                 // rows of a workgroup, kClipRows at most
 };
 hipError_t run_qk_clip(const ClipArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
 hipError_t run_reset_logits(const ClipArgs& a, hipStream_t st);
-// Rows of a weight one workgroup of the clip takes.
-constexpr int kClipRows = 8;
+// Rows of its entry one workgroup of the clip takes: 16 where that still makes
+// 1024 workgroups, else 4, one a wave (on an MI355X 32 layers of 4096 + 1024
+// rows of 4096 bf16 take 113 us with 16 rows, 130 with 8; one of 1024 rows of
+// 768 fp32 7.6 us with 16, 4.6 with 4).
+constexpr int kClipRows = 16, kClipRowsFew = 4;
 
 }  // namespace muon

@@ -566,46 +566,69 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, i
   }
 }
 
-// Joins the splits: one wave a row.
+// Joins the splits: a workgroup a row, 32 lanes along the head (4 elements
+// each) times 8 parts of the splits, summed through LDS in a fixed order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (row >= all) return;
+  __shared__ float4 sums[8][32];
+  __shared__ float mx[8], ls[8];
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens, row = blockIdx.x;
   const int i = static_cast<int>(row % a.seqs.q_tokens);
   const int64_t bh = row / a.seqs.q_tokens;
   const int head = static_cast<int>(bh % a.q_heads), b = static_cast<int>(bh / a.q_heads);
   const bool live = !a.seqs.q_len || i < a.seqs.q_len[b];
+  const int d = 4 * lane;
+  // the part's own maximum and sums
   float m = -kInf;
-  for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, a.part_ml[s * all + row].x);
-  m = wave_max(m);
-  const float mu = m == -kInf ? 0.f : m;
+  for (int s = part; s < a.splits; s += 8) m = fmaxf(m, a.part_ml[s * all + row].x);
   float l = 0.f;
-  for (int s = lane; s < a.splits; s += 64) {
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = part; s < a.splits; s += 8) {
     const float2 v = a.part_ml[s * all + row];
-    l += v.y * exp2_(v.x - mu);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
-  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
-  char* orow = at_row_w(a.out, b, i, head);
-  char* rrow = a.res.p ? at_row_w(a.res, b, i, head) : nullptr;
-  for (int d = lane; d < a.dim; d += 64) {
-    float x = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float w = exp2_(a.part_ml[s * all + row].x - mu);
-      if (w != 0.f) x = fmaf(w, a.part_o[(s * all + row) * a.dim + d], x);
+    if (v.x == -kInf) continue;  // a part that sees nothing
+    const float w = exp2_(v.x - m);
+    l = fmaf(w, v.y, l);
+    if (d < a.dim) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (s * all + row) * a.dim + d);
+      x.x = fmaf(w, y.x, x.x); x.y = fmaf(w, y.y, x.y); x.z = fmaf(w, y.z, x.z); x.w = fmaf(w, y.w, x.w);
     }
-    x = live ? x * inv : 0.f;
-    const T y = from_f32<T>(x);
-    reinterpret_cast<T*>(orow)[d] = y;
-    if constexpr (sizeof(T) == 2)
-      if (rrow) reinterpret_cast<T*>(rrow)[d] = from_f32<T>(x - to_f32<T>(y));
   }
+  sums[part][lane] = x;
+  if (lane == 0) { mx[part] = m; ls[part] = l; }
+  __syncthreads();
+  if (part != 0) return;
+  m = mx[0];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) m = fmaxf(m, mx[k]);
+  l = 0.f;
+  x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float w = mx[k] == -kInf ? 0.f : exp2_(mx[k] - m);
+    const float4 y = sums[k][lane];
+    l = fmaf(w, ls[k], l);
+    x.x = fmaf(w, y.x, x.x); x.y = fmaf(w, y.y, x.y); x.z = fmaf(w, y.z, x.z); x.w = fmaf(w, y.w, x.w);
+  }
+  const bool some = live && l != 0.f;
   if (lane == 0) {
-    a.lse[row] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
-    if (a.max_logits && live && m > -kInf) atomic_max_f32(a.max_logits + head, m * kLn2);
+    a.lse[row] = some ? (m + __log2f(l)) * kLn2 : -kInf;
+    if (a.max_logits && some && m > -kInf) atomic_max_f32(a.max_logits + head, m * kLn2);
+  }
+  if (d >= a.dim) return;
+  const float inv = some ? 1.f / l : 0.f;
+  float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+  if (!some) o[0] = o[1] = o[2] = o[3] = 0.f;
+  char* orow = at_row_w(a.out, b, i, head);
+  if constexpr (sizeof(T) == 2) {
+    const uint2 w = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+    *reinterpret_cast<uint2*>(orow + 2 * d) = w;
+    if (a.res.p)
+      *reinterpret_cast<uint2*>(at_row_w(a.res, b, i, head) + 2 * d) =
+          make_uint2(pack_bf16x2(o[0] - __uint_as_float(w.x << 16), o[1] - __uint_as_float(w.x & 0xffff0000u)),
+                     pack_bf16x2(o[2] - __uint_as_float(w.y << 16), o[3] - __uint_as_float(w.y & 0xffff0000u)));
+  } else {
+    *reinterpret_cast<float4*>(orow + 4 * d) = make_float4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -999,6 +1022,53 @@ __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
 // through LDS to every head.  HBM-bound: each element is read and written
 // once.
 // ---------------------------------------------------------------------------
+// Unit u of a head: a piece that turns (u < turning), else one that is copied.
+template <typename T>
+__device__ __forceinline__ void rotary_unit(const RotaryArgs& a, const T* x, T* y, const float2* w, int u, int turning,
+                                            bool vec) {
+  constexpr int EPC = 16 / sizeof(T);
+  const int half = a.rot / 2, width = vec ? EPC : 1;
+  if (u >= turning) {
+    const int d = a.rot + (u - turning) * width;
+    if (vec) *reinterpret_cast<u32x4_t*>(y + d) = *reinterpret_cast<const u32x4_t*>(x + d);
+    else y[d] = x[d];
+  } else if (!vec) {
+    const int p = a.interleaved ? 2 * u : u, q = a.interleaved ? p + 1 : u + half;
+    const float c = w[u].x, sn = w[u].y, e = to_f32<T>(x[p]), f = to_f32<T>(x[q]);
+    y[p] = from_f32<T>(e * c - f * sn);
+    y[q] = from_f32<T>(e * sn + f * c);
+  } else {
+    // a piece of EPC elements: pairs of it (interleaved), or it and the piece
+    // half a rotation further
+    float e[8], f[8];
+    if constexpr (sizeof(T) == 2) load8(x, u * EPC, e);
+    else *reinterpret_cast<float4*>(e) = *reinterpret_cast<const float4*>(x + u * EPC);
+    if (a.interleaved) {
+#pragma unroll
+      for (int q = 0; q < EPC / 2; ++q) {
+        const float2 cw = w[u * (EPC / 2) + q];
+        const float g = e[2 * q], h = e[2 * q + 1];
+        e[2 * q] = g * cw.x - h * cw.y;
+        e[2 * q + 1] = g * cw.y + h * cw.x;
+      }
+    } else {
+      if constexpr (sizeof(T) == 2) load8(x, u * EPC + half, f);
+      else *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(x + u * EPC + half);
+#pragma unroll
+      for (int q = 0; q < EPC; ++q) {
+        const float2 cw = w[u * EPC + q];
+        const float g = e[q], h = f[q];
+        e[q] = g * cw.x - h * cw.y;
+        f[q] = g * cw.y + h * cw.x;
+      }
+      if constexpr (sizeof(T) == 2) store8(y, u * EPC + half, f);
+      else *reinterpret_cast<float4*>(y + u * EPC + half) = *reinterpret_cast<const float4*>(f);
+    }
+    if constexpr (sizeof(T) == 2) store8(y, u * EPC, e);
+    else *reinterpret_cast<float4*>(y + u * EPC) = *reinterpret_cast<const float4*>(e);
+  }
+}
+
 constexpr int kRotPairs = 512;  // angles of a workgroup
 template <typename T>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int per_block) {
@@ -1027,59 +1097,28 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int per_block) {
     const int width = vec ? EPC : 1;
     const int turning = (a.interleaved ? a.rot / (vec ? EPC : 2) : half / width);
     const int units = turning + (same ? 0 : (a.dim - a.rot) / width);
-    const int total = n * t.heads * units;
-    for (int i = threadIdx.x; i < total; i += 256) {
-      const int u = i % units, th = i / units, head = th % t.heads, tk = th / t.heads;
-      const int64_t tok = first + tk, b = tok / a.tokens, at = tok % a.tokens;
+    if (units == 0 || t.heads == 0) continue;
+    // unit u of head `head` of token tk, by steps of 256 units
+    int u = threadIdx.x % units, head = threadIdx.x / units, tk = head / t.heads;
+    head -= tk * t.heads;
+    const int du = 256 % units, dh = 256 / units % t.heads, dt = 256 / units / t.heads;
+    while (tk < n) {
+      const int64_t tok = first + tk, b = tok / a.tokens, at = tok - b * a.tokens;
       const T* x = reinterpret_cast<const T*>(t.x.p + b * t.x.batch + at * t.x.token + head * t.x.head);
       T* y = reinterpret_cast<T*>(t.y.p + b * t.y.batch + at * t.y.token + head * t.y.head);
-      const float2* w = turn + tk * half;
-      if (u >= turning) {
-        const int d = a.rot + (u - turning) * width;
-        if (vec) *reinterpret_cast<u32x4_t*>(y + d) = *reinterpret_cast<const u32x4_t*>(x + d);
-        else y[d] = x[d];
-      } else if (!vec) {
-        const int p = a.interleaved ? 2 * u : u, q = a.interleaved ? p + 1 : u + half;
-        const float c = w[u].x, sn = w[u].y, e = to_f32<T>(x[p]), f = to_f32<T>(x[q]);
-        y[p] = from_f32<T>(e * c - f * sn);
-        y[q] = from_f32<T>(e * sn + f * c);
-      } else {
-        // a piece of EPC elements: pairs of it (interleaved), or it and the
-        // piece half a rotation further
-        float e[8], f[8];
-        if constexpr (sizeof(T) == 2) load8(x, u * EPC, e);
-        else *reinterpret_cast<float4*>(e) = *reinterpret_cast<const float4*>(x + u * EPC);
-        if (a.interleaved) {
-#pragma unroll
-          for (int q = 0; q < EPC / 2; ++q) {
-            const float2 cw = w[u * (EPC / 2) + q];
-            const float g = e[2 * q], h = e[2 * q + 1];
-            e[2 * q] = g * cw.x - h * cw.y;
-            e[2 * q + 1] = g * cw.y + h * cw.x;
-          }
-        } else {
-          if constexpr (sizeof(T) == 2) load8(x, u * EPC + half, f);
-          else *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(x + u * EPC + half);
-#pragma unroll
-          for (int q = 0; q < EPC; ++q) {
-            const float2 cw = w[u * EPC + q];
-            const float g = e[q], h = f[q];
-            e[q] = g * cw.x - h * cw.y;
-            f[q] = g * cw.y + h * cw.x;
-          }
-          if constexpr (sizeof(T) == 2) store8(y, u * EPC + half, f);
-          else *reinterpret_cast<float4*>(y + u * EPC + half) = *reinterpret_cast<const float4*>(f);
-        }
-        if constexpr (sizeof(T) == 2) store8(y, u * EPC, e);
-        else *reinterpret_cast<float4*>(y + u * EPC) = *reinterpret_cast<const float4*>(e);
-      }
+      rotary_unit<T>(a, x, y, turn + tk * half, u, turning, vec);
+      u += du;
+      head += dh;
+      tk += dt;
+      if (u >= units) { u -= units; ++head; }
+      if (head >= t.heads) { head -= t.heads; ++tk; }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// The clip.  A workgroup has kClipRows rows of one weight; rows whose factor is
-// 1 are not touched.  HBM-bound on the rows that change.
+// The clip.  A workgroup has a few rows of one entry; rows whose factor is 1
+// are not touched.  HBM-bound on the rows that change.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float clip_gamma(float m, float threshold) {
   return m > threshold && m < kInf ? threshold / m : 1.f;
@@ -1087,38 +1126,59 @@ __device__ __forceinline__ float clip_gamma(float m, float threshold) {
 template <typename T>
 __global__ __launch_bounds__(256) void k_qk_clip(ClipArgs a) {
   constexpr int EPC = 16 / sizeof(T);
+  __shared__ float factor[kClipRows];
   int k = 0;
-  while (k + 1 < a.n && a.first[k + 1] <= static_cast<int>(blockIdx.x)) ++k;
+  for (int step = kClipMax / 2; step > 0; step /= 2)  // the last entry that starts at or before this workgroup
+    if (k + step < a.n && a.first[k + step] <= static_cast<int>(blockIdx.x)) k += step;
   const ClipEntry& e = a.e[k];
   const int lane = threadIdx.x & 63, group = e.q_heads / e.kv_heads;
   const int rows_q = e.q_heads * e.dim, rows = rows_q + e.kv_heads * e.dim;
-  const int base = (blockIdx.x - a.first[k]) * kClipRows;
-  for (int i = threadIdx.x >> 6; i < kClipRows; i += 4) {
+  const int base = (blockIdx.x - a.first[k]) * a.rows;
+  bool any = false;
+  if (threadIdx.x < a.rows) {
+    const int row = base + threadIdx.x;
+    float f = 1.f;
+    if (row < rows) {
+      const bool is_q = row < rows_q;
+      const int head = (is_q ? row : row - rows_q) / e.dim, kvh = is_q ? head / group : head;
+      float least = 1.f;
+      for (int g = 0; g < group; ++g) least = fminf(least, clip_gamma(e.logits[kvh * group + g], e.threshold));
+      const float key = sqrtf(least);
+      f = is_q ? clip_gamma(e.logits[head], e.threshold) / key : key;
+    }
+    factor[threadIdx.x] = f;
+    any = f != 1.f;
+  }
+  if (!__syncthreads_or(any)) return;
+  for (int i = threadIdx.x >> 6; i < a.rows; i += 4) {
     const int row = base + i;
-    if (row >= rows) return;
-    const bool is_q = row < rows_q;
-    const int at = is_q ? row : row - rows_q, head = at / e.dim, kvh = is_q ? head / group : head;
-    float least = 1.f;
-    for (int g = 0; g < group; ++g) least = fminf(least, clip_gamma(e.logits[kvh * group + g], e.threshold));
-    const float key = sqrtf(least);
-    const float f = is_q ? clip_gamma(e.logits[head], e.threshold) / key : key;
+    const float f = factor[i];
     if (f == 1.f) continue;
+    const bool is_q = row < rows_q;
+    const int at = is_q ? row : row - rows_q;
     T* w = reinterpret_cast<T*>(is_q ? e.wq + at * e.ldq : e.wk + at * e.ldk);
     int done = 0;
     if (e.vec) {
-      done = e.cols / EPC * EPC;
-      for (int c = lane * EPC; c < done; c += 64 * EPC) {
-        float x[8];
-        if constexpr (sizeof(T) == 2) {
-          load8(w, c, x);
+      const int chunks = e.cols / EPC;
+      done = chunks * EPC;
+      u32x4_t* const w16 = reinterpret_cast<u32x4_t*>(w);
+      for (int c = lane; c < chunks; c += 8 * 64) {
+        u32x4_t v[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) x[q] *= f;
-          store8(w, c, x);
-        } else {
-          float4 v = *reinterpret_cast<const float4*>(w + c);
-          v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-          *reinterpret_cast<float4*>(w + c) = v;
-        }
+        for (int q = 0; q < 8; ++q)
+          if (c + q * 64 < chunks) v[q] = w16[c + q * 64];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (c + q * 64 < chunks) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if constexpr (sizeof(T) == 2)
+                v[q][x] = pack_bf16x2(__uint_as_float(v[q][x] << 16) * f, __uint_as_float(v[q][x] & 0xffff0000u) * f);
+              else
+                v[q][x] = __float_as_uint(__uint_as_float(v[q][x]) * f);
+            }
+            w16[c + q * 64] = v[q];
+          }
       }
     }
     for (int c = done + lane; c < e.cols; c += 64) w[c] = from_f32<T>(to_f32<T>(w[c]) * f);
@@ -1155,7 +1215,7 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
-  hipLaunchKernelGGL((k_attn_join<T>), dim3(static_cast<unsigned>((rows + 3) / 4)), b, 0, st, a);
+  hipLaunchKernelGGL((k_attn_join<T>), dim3(static_cast<unsigned>(rows)), b, 0, st, a);
   return hipGetLastError();
 }
 
