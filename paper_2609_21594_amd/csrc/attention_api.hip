@@ -133,8 +133,8 @@ muon_status_t check_sizes(const muon_attention_t* a, Why& why) {
   // more a sequence, and 8 or more rows a workgroup in the passes over rows
   const double rows = double(a->batch) * a->q_heads * double(std::max(a->q_tokens, a->k_tokens));
   const double tiles = rows / 128 + double(a->batch) * a->q_heads * double(a->sequences + 1);
-  if (rows > double(1 << 26) || tiles > double(1 << 23))
-    return why.fail(MUON_ERR_UNSUPPORTED, "too many rows in one call (heads x tokens: at most 2^26)");
+  if (rows > double(1 << 25) || tiles > double(1 << 23))
+    return why.fail(MUON_ERR_UNSUPPORTED, "too many rows in one call (heads x tokens: at most 2^25)");
   return MUON_OK;
 }
 
@@ -153,29 +153,37 @@ int32_t window_of(const muon_attention_t* a) {  // one beyond every gap is none
 }
 
 struct ScratchPlan {
-  int splits = 1;
-  bool kv_split = false;
-  size_t part_o = 0, part_ml = 0, lse2 = 0, delta = 0, dk = 0, dv = 0, bytes = 0;
+  int splits = 1, kv_parts = 1;
+  size_t part_o = 0, part_ml = 0, lse2 = 0, delta = 0, dk = 0, dv = 0;
+  size_t sq = 0, sk = 0, sv = 0, sdo = 0, bytes = 0;
 };
 ScratchPlan plan_scratch(const muon_attention_t* a, bool backward) {
   ScratchPlan p;
   const muon::Seqs s = seqs_of(a);
-  const size_t rows = size_t(a->batch) * size_t(a->q_heads) * size_t(a->q_tokens);
+  const int64_t rows = a->batch * a->q_heads * a->q_tokens, keys = a->batch * a->kv_heads * a->k_tokens;
   const auto take = [&](size_t& at, size_t bytes) { at = p.bytes; p.bytes += up256(bytes); };
+  if (rows == 0 && (!backward || keys == 0)) return p;
   if (!backward) {
-    p.splits = muon::forward_splits(s, a->q_heads, a->kv_heads, a->head_dim, a->dtype, a->causal != 0, window_of(a));
+    p.splits = muon::forward_splits(s, a->q_heads, a->kv_heads, a->causal != 0, window_of(a));
     if (p.splits > 1) {
-      take(p.part_o, rows * size_t(p.splits) * size_t(a->head_dim) * 4);
-      take(p.part_ml, rows * size_t(p.splits) * 8);
+      take(p.part_o, size_t(rows) * size_t(p.splits) * size_t(a->head_dim) * 4);
+      take(p.part_ml, size_t(rows) * size_t(p.splits) * 8);
     }
   } else {
-    take(p.lse2, rows * 4);
-    take(p.delta, rows * 4);
-    p.kv_split = muon::backward_splits_heads(s, a->q_heads, a->kv_heads, a->head_dim, a->dtype);
-    if (p.kv_split) {
-      const size_t n = size_t(a->batch) * size_t(a->k_tokens) * size_t(a->q_heads) * size_t(a->head_dim) * 4;
-      take(p.dk, n);
-      take(p.dv, n);
+    take(p.lse2, size_t(rows) * 4);
+    take(p.delta, size_t(rows) * 4);
+    p.kv_parts = muon::backward_parts(s, a->q_heads, a->kv_heads);
+    if (p.kv_parts > 1) {
+      take(p.dk, size_t(keys) * size_t(p.kv_parts) * size_t(a->head_dim) * 4);
+      take(p.dv, size_t(keys) * size_t(p.kv_parts) * size_t(a->head_dim) * 4);
+    }
+  }
+  if (a->dtype == MUON_F32) {
+    take(p.sk, muon::split_bytes(keys, a->head_dim));
+    take(p.sv, muon::split_bytes(keys, a->head_dim));
+    if (backward) {
+      take(p.sq, muon::split_bytes(rows, a->head_dim));
+      take(p.sdo, muon::split_bytes(rows, a->head_dim));
     }
   }
   return p;
@@ -258,7 +266,7 @@ muon_status_t check_attention(const muon_attention_t* a, const muon_attention_gr
   k.scale = a->scale;
   k.scale2 = float(double(a->scale) * 1.4426950408889634074);
   k.splits = p.splits;
-  k.kv_split = p.kv_split;
+  k.kv_parts = p.kv_parts;
   char* const s = static_cast<char*>(a->scratch);
   const auto part = [&](size_t at) { return reinterpret_cast<float*>(s + at); };
   if (p.splits > 1) {
@@ -268,7 +276,11 @@ muon_status_t check_attention(const muon_attention_t* a, const muon_attention_gr
   if (g) {
     k.lse2 = part(p.lse2);
     k.delta = part(p.delta);
-    if (p.kv_split) { k.part_dk = part(p.dk); k.part_dv = part(p.dv); }
+    if (p.kv_parts > 1) { k.part_dk = part(p.dk); k.part_dv = part(p.dv); }
+  }
+  if (a->dtype == MUON_F32) {
+    k.split_k = s + p.sk; k.split_v = s + p.sv;
+    k.split_q = s + p.sq; k.split_do = s + p.sdo;
   }
   return MUON_OK;
 }

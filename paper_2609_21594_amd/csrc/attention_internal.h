@@ -43,19 +43,28 @@ struct AttnArgs {
   // backward: per row log2(sum exp) (+inf where nothing is visible) and
   // dout . out
   float *lse2, *delta;
-  // backward, heads of a group in workgroups of their own: fp32 gradients per
-  // query head, [batch * k_tokens][q_heads][dim] (packed: [k_tokens][..])
-  int32_t kv_split;
+  // backward, the heads of a group in kv_parts parts with workgroups of their
+  // own: where more than one, the parts' fp32 gradients,
+  // [batch * k_tokens][kv_heads][kv_parts][dim]
+  int32_t kv_parts;
   float *part_dk, *part_dv;
+  // fp32: the planes of the arrays that tiles are staged from (k_split)
+  char *split_q, *split_k, *split_v, *split_do;
+  // what the tiles are staged from, and bytes between a row's planes (set by
+  // the launch)
+  Heads sq, sk, sv, sdo;
+  int32_t plane;
 };
+// Bytes of the planes of an fp32 array of `rows` rows.
+inline size_t split_bytes(int64_t rows, int dim) { return size_t(rows) * size_t((dim + 7) / 8) * 48; }
 
-hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
-hipError_t run_attention_backward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer);
+hipError_t run_attention_forward(AttnArgs a, int dtype, hipStream_t st, LaunchTimer* timer);
+hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchTimer* timer);
 // Over how many parts of the key axis the forward pass of this request is
-// spread (1: none), and whether its backward pass gives every query head
-// workgroups of its own for the key and value gradients.
-int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype, bool causal, int window);
-bool backward_splits_heads(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype);
+// spread (1: none), and in how many parts its backward pass takes the query
+// heads that share keys.
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window);
+int backward_parts(const Seqs& s, int q_heads, int kv_heads);
 
 constexpr int kRotaryMax = 4;
 struct RotaryTensor {

@@ -70,13 +70,13 @@ __device__ __forceinline__ void wave_priority() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Tiles of heads of up to DU elements, in rows of DP (a power of two).
-template <typename T, int DU>
+// Tiles of heads of up to DU elements, in rows of DP bf16 (a power of two).
+template <int DU>
 struct Lay {
   static constexpr int DP = DU <= 64 ? 64 : 128;
-  static constexpr int ES = sizeof(T), EPC = 16 / ES, CH = DP / EPC, RB = DP * ES;
-  static constexpr int STEPS = DU / EPC / 2;  // MFMA steps over the head: 2 chunks each, one per half of the wave
-  static constexpr int DB = DU / 32;          // 32-row blocks of the head
+  static constexpr int CH = DP / 8, RB = DP * 2;  // 16-byte chunks and bytes of a row
+  static constexpr int STEPS = DU / 16;           // MFMA steps over the head: 2 chunks each, one per half of the wave
+  static constexpr int DB = DU / 32;              // 32-row blocks of the head
   __device__ __forceinline__ static constexpr int key(int r) {
     if constexpr (CH == 8) return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3);
     else return ((r & 3) << 2) | ((r >> 2) & 3);
@@ -84,123 +84,193 @@ struct Lay {
   __device__ __forceinline__ static int at(int r, int c) { return r * RB + ((c ^ key(r)) << 4); }
 };
 
+// The products' operands: bf16 (PL = 1), or fp32 values as the exact sum of
+// PL = 3 bf16 planes, x = h + m + l (each the rounding of what the ones before
+// it leave; 8 bits each, so 24 in all unless l falls below bf16's range, from
+// |x| < 2^-109 on).  A product of two such values is hh + hm + mh + mm + hl +
+// lh, six bf16 MFMAs in fp32 accumulation; what is left out is 2^-24 of it.
+// (fp32 MFMAs have a sixteenth of the bf16 rate, so this is 2.7 times theirs.)
+template <int PL> struct Io { using T = uint16_t; };
+template <> struct Io<3> { using T = float; };
+template <int PL> struct Frag { u32x4_t v[PL]; };
+template <int PL>
+__device__ __forceinline__ void mma(const Frag<PL>& a, const Frag<PL>& b, f32x16_t& c) {
+  if constexpr (PL == 3) {
+    Mma<uint16_t>::run(a.v[1], b.v[1], c);
+    Mma<uint16_t>::run(a.v[0], b.v[2], c);
+    Mma<uint16_t>::run(a.v[2], b.v[0], c);
+    Mma<uint16_t>::run(a.v[0], b.v[1], c);
+    Mma<uint16_t>::run(a.v[1], b.v[0], c);
+  }
+  Mma<uint16_t>::run(a.v[0], b.v[0], c);
+}
+// A pair of values as words of the planes.
+template <int PL>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t* w) {
+  w[0] = pack_bf16x2(x, y);
+  if constexpr (PL == 3) {
+    x -= __uint_as_float(w[0] << 16);
+    y -= __uint_as_float(w[0] & 0xffff0000u);
+    w[1] = pack_bf16x2(x, y);
+    x -= __uint_as_float(w[1] << 16);
+    y -= __uint_as_float(w[1] & 0xffff0000u);
+    w[2] = pack_bf16x2(x, y);
+  }
+}
+
 // LDS by byte address.
 typedef const __attribute__((address_space(3))) u32x4_t* lds_u32x4_p;
-typedef const __attribute__((address_space(3))) uint32_t* lds_u32_p;
 __device__ __forceinline__ u32x4_t lds16(uint32_t at) { return *reinterpret_cast<lds_u32x4_p>(at); }
-__device__ __forceinline__ uint32_t lds4(uint32_t at) { return *reinterpret_cast<lds_u32_p>(at); }
 __device__ __forceinline__ uint2 lds_tr8(uint32_t at) {
   typedef short v4i16 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(
       uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) v4i16*>(at)));
 }
 
-// Stages ROWS rows of `dch` chunks into LDS by direct loads of the whole
-// workgroup of 256.  Rows beyond the sequence repeat its last one and chunks
-// from dch on the last one: what they hold is finite where the operand is, and
-// meets zeros or is never read.  Load i of a thread has the row of load 0 plus
-// i * STEP; where 16 divides STEP (or 2 STEP) its chunk, and so its 32-bit
-// offset, is that of load 0 (or of load i % 2) plus a scalar.
-template <typename T, int DP, int ROWS>
+// Stages ROWS rows of `dch` chunks, plane by plane, into LDS by direct loads of
+// the whole workgroup of 256.  Rows beyond the sequence repeat its last one and
+// chunks from dch on the last one: what they hold is finite where the operand
+// is, and meets zeros or is never read.  Load i of a thread has the row of load
+// 0 plus i * STEP; 16 divides STEP, so its chunk is that of load 0, and its
+// 32-bit offset that of load 0 plus a scalar.
+template <int PL, int DU, int ROWS>
 struct Stager {
-  using L = Lay<T, DP>;
-  static constexpr int STEP = 256 / L::CH, N = ROWS * L::CH / 256, NOFF = STEP % 16 == 0 ? 1 : 2;
-  static_assert(ROWS * L::CH % 256 == 0 && NOFF * STEP % 16 == 0 && (N % NOFF == 0), "whole loads");
-  uint32_t off[NOFF];
-  uint32_t stride;
+  using L = Lay<DU>;
+  static constexpr int STEP = 256 / L::CH, N = ROWS * L::CH / 256;
+  static_assert(ROWS * L::CH % 256 == 0 && STEP % 16 == 0, "whole loads");
+  uint32_t off, stride;
   __device__ __forceinline__ void init(uint32_t stride_, int dch) {
     stride = stride_;
-#pragma unroll
-    for (int i = 0; i < NOFF; ++i) {
-      const int r = threadIdx.x / L::CH + i * STEP;
-      off[i] = r * stride + chunk(r, dch) * 16;
-    }
+    off = threadIdx.x / L::CH * stride + chunk(dch) * 16;
   }
-  __device__ __forceinline__ static int chunk(int r, int dch) {
-    return min((static_cast<int>(threadIdx.x) % L::CH) ^ L::key(r), dch - 1);
+  __device__ __forceinline__ static int chunk(int dch) {
+    return min((static_cast<int>(threadIdx.x) % L::CH) ^ L::key(threadIdx.x / L::CH), dch - 1);
   }
-  // base: row 0 of the tile; left: rows from there to the sequence's end.
-  __device__ __forceinline__ void issue(const char* base, int left, int dch, uint32_t lds, int wave) const {
+  // base: row 0 of the tile; plane: bytes from one plane of a row to the next;
+  // left: rows from there to the sequence's end.
+  __device__ __forceinline__ void issue(const char* base, int plane, int left, int dch, uint32_t lds, int wave) const {
     if (left >= ROWS) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        load_lds16(base + static_cast<int64_t>(i / NOFF * NOFF * STEP) * stride, off[i % NOFF], lds + (i * 256 + wave * 64) * 16);
+      for (int p = 0; p < PL; ++p)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          load_lds16(base + p * plane + static_cast<int64_t>(i * STEP) * stride, off,
+                     lds + p * ROWS * L::RB + (i * 256 + wave * 64) * 16);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int r = threadIdx.x / L::CH + i * STEP;
-        load_lds16(base, static_cast<uint32_t>(min(r, left - 1)) * stride + chunk(r, dch) * 16,
-                   lds + (i * 256 + wave * 64) * 16);
+        const uint32_t at = static_cast<uint32_t>(min(static_cast<int>(threadIdx.x) / L::CH + i * STEP, left - 1)) * stride +
+                            chunk(dch) * 16;
+#pragma unroll
+        for (int p = 0; p < PL; ++p)
+          load_lds16(base + p * plane, at, lds + p * ROWS * L::RB + (i * 256 + wave * 64) * 16);
       }
     }
   }
 };
 
-// The lane's row of an operand kept in registers: chunks 2 s + half, zeros
-// beyond the head.
-template <typename T, int DP>
-__device__ __forceinline__ void load_operand(const char* row, int dch, int half, u32x4_t* f) {
-  using L = Lay<T, DP>;
+// 8 elements from c * 8 on of a row (zeros from `dim` on), as operand planes.
+template <int PL>
+__device__ __forceinline__ Frag<PL> load_chunk(const char* row, int c, int dim) {
+  Frag<PL> f;
+  if constexpr (PL == 1) {
+    f.v[0] = 8 * c < dim ? *reinterpret_cast<const u32x4_t*>(row + c * 16) : u32x4_t{0, 0, 0, 0};
+  } else {
+    float x[8] = {};
+    if (8 * c < dim) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(row + c * 32);
+    if (8 * c + 4 < dim) *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(row + c * 32 + 16);
 #pragma unroll
-  for (int s = 0; s < L::STEPS; ++s) {
-    const int c = 2 * s + half;
-    f[s] = c < dch ? *reinterpret_cast<const u32x4_t*>(row + c * 16) : u32x4_t{0, 0, 0, 0};
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w[3];
+      split_pair<PL>(x[2 * k], x[2 * k + 1], w);
+#pragma unroll
+      for (int p = 0; p < PL; ++p) f.v[p][k] = w[p];
+    }
   }
+  return f;
+}
+// The lane's row of an operand kept in registers: chunks 2 s + half.
+template <int PL, int DU>
+__device__ __forceinline__ void load_operand(const char* row, int dim, int half, Frag<PL>* f) {
+#pragma unroll
+  for (int s = 0; s < Lay<DU>::STEPS; ++s) f[s] = load_chunk<PL>(row, 2 * s + half, dim);
+}
+// The lane's half of the sum over the head of x * y, both as stored.
+template <int PL, int DU>
+__device__ __forceinline__ float dot_rows(const char* x, const char* y, int dim, int half) {
+  float r = 0.f;
+#pragma unroll
+  for (int s = 0; s < Lay<DU>::STEPS; ++s) {
+    const int c = 2 * s + half;
+    if constexpr (PL == 1) {
+      if (8 * c >= dim) continue;
+      const u32x4_t a = *reinterpret_cast<const u32x4_t*>(x + c * 16), b = *reinterpret_cast<const u32x4_t*>(y + c * 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        r = fmaf(__uint_as_float(a[k] << 16), __uint_as_float(b[k] << 16), r);
+        r = fmaf(__uint_as_float(a[k] & 0xffff0000u), __uint_as_float(b[k] & 0xffff0000u), r);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (8 * c + 4 * q >= dim) continue;
+        const float4 a = *reinterpret_cast<const float4*>(x + c * 32 + q * 16), b = *reinterpret_cast<const float4*>(y + c * 32 + q * 16);
+        r = fmaf(a.x, b.x, r); r = fmaf(a.y, b.y, r); r = fmaf(a.z, b.z, r); r = fmaf(a.w, b.w, r);
+      }
+    }
+  }
+  return r;
 }
 
 // A operand of the contraction over the head: rows r0 + lane % 32 of a tile,
 // chunks 2 st + half.  As 2 st has no bit in common with half, the swizzled
 // address is a lane's base with bits flipped by a constant, plus a constant:
 // `base` is rows_base + the tile's address (a multiple of 1024, so that the
-// flipped bits are the lane's own), `off` the rest.
-template <typename T, int DP>
+// flipped bits are the lane's own), `off` the rest; PLANE: bytes of a plane.
+template <int DU>
 __device__ __forceinline__ uint32_t rows_base(int lane) {
-  return Lay<T, DP>::at(lane & 31, lane >> 5);
+  return Lay<DU>::at(lane & 31, lane >> 5);
 }
-template <typename T, int DP>
-__device__ __forceinline__ u32x4_t frag_rows(uint32_t base, int off, int st) {
-  return lds16((base ^ (st << 5)) + off);
-}
-// Steps of a contraction over 32 tile rows: 16 rows each (bf16), 8 (fp32).
-template <typename T> constexpr int kRowSteps = sizeof(T) == 2 ? 2 : 4;
-// A operand of the contraction over tile rows: elements 32 db + lane % 32 of
-// the rows that step `st` of accumulator block rows r0 .. r0 + 31 holds (r0 a
-// multiple of 32, in `off`).  Rows further by 4, 8 or 16 flip key bits in the
-// same way.
-template <typename T, int DP>
-__device__ __forceinline__ uint32_t cols_base(int lane) {
-  using L = Lay<T, DP>;
-  if constexpr (sizeof(T) == 2) {
-    const int G = lane >> 4, q = lane & 15;
-    return L::at(4 * (G >> 1) + (q >> 2), 2 * (G & 1) + ((q & 3) >> 1)) + (q & 1) * 8;
-  } else {
-    return L::at(4 * (lane >> 5), (lane & 31) >> 2) + (lane & 3) * 4;
-  }
-}
-template <typename T, int DP>
-__device__ __forceinline__ u32x4_t frag_cols(uint32_t base, int off, int st, int db) {
-  using L = Lay<T, DP>;
-  if constexpr (sizeof(T) == 2) {
-    constexpr int flip = L::key(8) << 4;
-    const uint32_t b = base ^ (db << 6);
-    const uint2 lo = lds_tr8(b + (off + 16 * st * L::RB)), hi = lds_tr8((b ^ flip) + (off + (16 * st + 8) * L::RB));
-    return u32x4_t{lo.x, lo.y, hi.x, hi.y};
-  } else {
-    u32x4_t f;
+template <int PL, int PLANE>
+__device__ __forceinline__ Frag<PL> frag_rows(uint32_t base, int off, int st) {
+  Frag<PL> f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      f[i] = lds4((base ^ ((db << 7) ^ (L::key(8 * (st & 1) + i) << 4))) + (off + (8 * st + i) * L::RB));
-    return f;
-  }
+  for (int p = 0; p < PL; ++p) f.v[p] = lds16((base ^ (st << 5)) + (off + p * PLANE));
+  return f;
 }
-// The B operand of that step: accumulator registers, rounded for bf16.
-template <typename T>
-__device__ __forceinline__ u32x4_t frag_acc(const f32x16_t& s, int st) {
-  u32x4_t f;
+// A operand of the contraction over tile rows: elements 32 db + lane % 32 of
+// the 16 rows that step `st` (of 2) of accumulator block rows r0 .. r0 + 31
+// holds (r0 a multiple of 32, in `off`).  Rows further by 8 flip key bits in
+// the same way.
+template <int DU>
+__device__ __forceinline__ uint32_t cols_base(int lane) {
+  const int G = lane >> 4, q = lane & 15;
+  return Lay<DU>::at(4 * (G >> 1) + (q >> 2), 2 * (G & 1) + ((q & 3) >> 1)) + (q & 1) * 8;
+}
+template <int PL, int DU, int PLANE>
+__device__ __forceinline__ Frag<PL> frag_cols(uint32_t base, int off, int st, int db) {
+  using L = Lay<DU>;
+  constexpr int flip = L::key(8) << 4;
+  const uint32_t b = base ^ (db << 6);
+  Frag<PL> f;
+#pragma unroll
+  for (int p = 0; p < PL; ++p) {
+    const int o = off + p * PLANE + 16 * st * L::RB;
+    const uint2 lo = lds_tr8(b + o), hi = lds_tr8((b ^ flip) + (o + 8 * L::RB));
+    f.v[p] = u32x4_t{lo.x, lo.y, hi.x, hi.y};
+  }
+  return f;
+}
+// The B operand of that step: accumulator registers, rounded or split.
+template <int PL>
+__device__ __forceinline__ Frag<PL> frag_acc(const f32x16_t& s, int st) {
+  Frag<PL> f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) f[i] = pack_bf16x2(s[8 * st + 2 * i], s[8 * st + 2 * i + 1]);
-    else f[i] = __float_as_uint(s[4 * st + i]);
+    uint32_t w[3];
+    split_pair<PL>(s[8 * st + 2 * i], s[8 * st + 2 * i + 1], w);
+#pragma unroll
+    for (int p = 0; p < PL; ++p) f.v[p][i] = w[p];
   }
   return f;
 }
@@ -217,7 +287,8 @@ __device__ __forceinline__ f32x16_t zero16() {
 // what the rounding took.  All lanes of the wave call it; `on`: this lane
 // writes.
 template <typename T, int DB>
-__device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row, char* res, int dch, int half, bool on) {
+__device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row, char* res, int dim, int half, bool on) {
+  const int dch = dim / (16 / static_cast<int>(sizeof(T)));
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
     if constexpr (sizeof(T) == 2) {
@@ -249,6 +320,34 @@ __device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row,
       }
     }
   }
+}
+
+// fp32 arrays that tiles are staged from, as planes: rows [batch][heads]
+// [tokens][3][head, padded to 8].  A thread has 8 elements.
+struct SplitArgs {
+  Heads from[4];
+  char* to[4];
+  int32_t tokens[4], heads[4];
+  int64_t first[5];   // first thread of each array
+  int32_t n, dim;
+};
+__global__ __launch_bounds__(256) void k_split(SplitArgs a) {
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (at >= a.first[a.n]) return;
+  int k = 0;
+  while (k + 1 < a.n && a.first[k + 1] <= at) ++k;
+  const int chunks = (a.dim + 7) / 8;
+  const int64_t i = at - a.first[k];
+  const int c = static_cast<int>(i % chunks);
+  const int64_t bth = i / chunks;  // heads vary fastest: reads are consecutive in the usual layout
+  const int head = static_cast<int>(bth % a.heads[k]);
+  const int64_t bt = bth / a.heads[k];
+  const int64_t b = bt / a.tokens[k], t = bt % a.tokens[k];
+  const Heads& h = a.from[k];
+  const Frag<3> f = load_chunk<3>(h.p + b * h.batch + t * h.token + head * h.head, c, a.dim);
+  char* to = a.to[k] + (((b * a.heads[k] + head) * a.tokens[k] + t) * 3 * chunks + c) * 16;
+#pragma unroll
+  for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4_t*>(to + p * chunks * 16) = f.v[p];
 }
 
 // ---------------------------------------------------------------------------
@@ -367,18 +466,19 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 }
 
 // ---------------------------------------------------------------------------
-// Forward.  A workgroup of 4 waves holds 128 NQ queries (32 NQ a wave) and
-// passes over the keys in tiles of BN, double-buffered in LDS, keeping the
-// running maximum and sum.
+// Forward.  A workgroup of 4 waves holds 128 queries (32 a wave) and passes
+// over the keys in tiles of BN, double-buffered in LDS, keeping the running
+// maximum and sum.
 // ---------------------------------------------------------------------------
-template <typename T, int DP, int NQ, int BN, bool SPLIT>
-__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
-  using L = Lay<T, DP>;
-  constexpr int BM = 128 * NQ, KB = BN / 32, TILE = BN * L::RB, STAGE = 2 * TILE;
+template <int PL, int DU, int BN, bool SPLIT>
+__global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
+  using L = Lay<DU>;
+  using T = typename Io<PL>::T;
+  constexpr int BM = 128, KB = BN / 32, PLANE = BN * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = a.dim / L::EPC;
+  const int dch = (a.dim + 7) / 8;
   int bid = blockIdx.x, split = 0;
   if constexpr (SPLIT) {
     const int items = gridDim.x / a.splits;
@@ -392,30 +492,24 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, i
 
   // the lane's rows.  pack: the rows are all heads of the group, each with all queries
   const int rows = pack ? s.q_rows * a.group : s.q_rows;
-  const int r0 = s.tile * BM + wave * 32 * NQ;
-  u32x4_t qf[NQ][L::STEPS];
-  int iq[NQ], head[NQ], jmin[NQ], jmax[NQ];
-  bool in[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int r = r0 + 32 * n + (lane & 31);
-    in[n] = r < rows;
-    iq[n] = min(r, rows - 1);
-    int g = it.g;
-    if (pack) {
-      g = iq[n] / s.q_rows;
-      iq[n] -= g * s.q_rows;
-    }
-    head[n] = it.kvh * a.group + g;
-    jmax[n] = a.causal ? min(s.nk - 1, iq[n] + shift) : s.nk - 1;
-    jmin[n] = a.causal && a.window ? max(0, iq[n] + shift - a.window + 1) : 0;
-    load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq[n], head[n]), dch, half, qf[n]);
+  const int r0 = s.tile * BM + wave * 32;
+  Frag<PL> qf[L::STEPS];
+  const int r = r0 + (lane & 31);
+  const bool in = r < rows;
+  int iq = min(r, rows - 1), g = it.g;
+  if (pack) {
+    g = iq / s.q_rows;
+    iq -= g * s.q_rows;
   }
+  const int head = it.kvh * a.group + g;
+  const int jmax = a.causal ? min(s.nk - 1, iq + shift) : s.nk - 1;
+  const int jmin = a.causal && a.window ? max(0, iq + shift - a.window + 1) : 0;
+  load_operand<PL, DU>(at_row(a.q, it.b, s.q0 + iq, head), a.dim, half, qf);
 
   // the keys of the workgroup and of the wave
   const int last = min(s.q_rows, s.nq) - 1;
   const KeyRange wg = pack ? keys_of(a, s, 0, last) : keys_of(a, s, s.tile * BM, min(s.tile * BM + BM - 1, last));
-  const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 32 * NQ - 1, last));
+  const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 31, last));
   int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
   if constexpr (SPLIT) {
     const int per = (max(t1 - t0, 0) + a.splits - 1) / a.splits;
@@ -424,28 +518,23 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, i
   }
 
   const uint32_t lds0 = lds_offset(smem);
-  const uint32_t rbase = lds0 + rows_base<T, DP>(lane), cbase = lds0 + cols_base<T, DP>(lane);
-  Stager<T, DP, BN> ks, vs;
-  ks.init(static_cast<uint32_t>(a.k.token), dch);
-  vs.init(static_cast<uint32_t>(a.v.token), dch);
-  const char* const krow = at_row(a.k, it.b, s.k0, it.kvh);
-  const char* const vrow = at_row(a.v, it.b, s.k0, it.kvh);
+  const uint32_t rbase = lds0 + rows_base<DU>(lane), cbase = lds0 + cols_base<DU>(lane);
+  Stager<PL, DU, BN> ks, vs;
+  ks.init(static_cast<uint32_t>(a.sk.token), dch);
+  vs.init(static_cast<uint32_t>(a.sv.token), dch);
+  const char* const krow = at_row(a.sk, it.b, s.k0, it.kvh);
+  const char* const vrow = at_row(a.sv, it.b, s.k0, it.kvh);
   auto issue = [&](int t) __attribute__((always_inline)) {
     const uint32_t at = lds0 + (t & 1) * STAGE;
     const int64_t j = t * BN;
-    ks.issue(krow + j * a.k.token, s.nk - t * BN, dch, at, wave);
-    vs.issue(vrow + j * a.v.token, s.nk - t * BN, dch, at + TILE, wave);
+    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * BN, dch, at, wave);
+    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * BN, dch, at + TILE, wave);
   };
 
-  f32x16_t o[NQ][L::DB];
-  float m[NQ], l[NQ], top[NQ];
+  f32x16_t o[L::DB];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-    for (int db = 0; db < L::DB; ++db) o[n][db] = zero16();
-    m[n] = top[n] = -kInf;
-    l[n] = 0.f;
-  }
+  for (int db = 0; db < L::DB; ++db) o[db] = zero16();
+  float m = -kInf, l = 0.f, top = -kInf;
   if (t0 < t1) issue(t0);
   for (int t = t0; t < t1; ++t) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -454,114 +543,96 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void k_attn_fwd(AttnArgs a, i
     const int j0 = t * BN;
     if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
     const uint32_t rb = rbase + (t & 1) * STAGE, cb = cbase + (t & 1) * STAGE;
-    f32x16_t p[NQ][KB];
+    f32x16_t p[KB];
     wave_priority<1>();
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) p[n][kb] = zero16();
+    for (int kb = 0; kb < KB; ++kb) p[kb] = zero16();
 #pragma unroll
     for (int st = 0; st < L::STEPS; ++st)
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const u32x4_t kf = frag_rows<T, DP>(rb, 32 * kb * L::RB, st);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) Mma<T>::run(kf, qf[n][st], p[n][kb]);
-      }
+      for (int kb = 0; kb < KB; ++kb) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * kb * L::RB, st), qf[st], p[kb]);
     wave_priority<0>();
-    const bool cut = j0 + BN > wv.all_end || j0 < wv.all_beg;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      if (cut) {
-        asm volatile("; a tile that the mask cuts");  // (a branch: else every tile pays for the comparisons)
-        const int lo = jmin[n] - j0 - 4 * half, hi = jmax[n] - j0 - 4 * half;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
-            if (j < lo || j > hi) p[n][kb][r] = -kInf;
-          }
-      }
-      float mx = -kInf;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[n][kb][r]);
-      mx = max32(mx);
-      top[n] = fmaxf(top[n], mx);
-      // Probabilities are taken relative to m, which follows the maximum only
-      // when that has grown by 2^kSlack: binary32 sums have room for the
-      // factor, bf16 rounds relatively, and most tiles leave o as it is.  (The
-      // parts of a split key axis report m as their maximum.)
-      const float mn = mx * a.scale2;
-      if (__any(mn > m[n] + (SPLIT ? 0.f : kSlack))) {
-        const float up = fmaxf(m[n], mn), alpha = m[n] == up ? 1.f : exp2_(m[n] - up);
-        m[n] = up;
-        l[n] *= alpha;
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[n][db][r] *= alpha;
-      }
-      const float mu = m[n] == -kInf ? 0.f : m[n];
-      float sum = 0.f;
+    if (j0 + BN > wv.all_end || j0 < wv.all_beg) {
+      asm volatile("; a tile that the mask cuts");  // (a branch: else every tile pays for the comparisons)
+      const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          p[n][kb][r] = exp2_(fmaf(p[n][kb][r], a.scale2, -mu));
-          sum += p[n][kb][r];
+          const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+          if (j < lo || j > hi) p[kb][r] = -kInf;
         }
-      l[n] += sum;
     }
+    float mx = -kInf;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[kb][r]);
+    mx = max32(mx);
+    top = fmaxf(top, mx);
+    // Probabilities are taken relative to m, which follows the maximum only
+    // when that has grown by 2^kSlack: binary32 sums have room for the factor,
+    // bf16 rounds relatively, and most tiles leave o as it is.  (The parts of a
+    // split key axis report m as their maximum.)
+    const float mn = mx * a.scale2;
+    if (__any(mn > m + (SPLIT ? 0.f : kSlack))) {
+      const float up = fmaxf(m, mn), alpha = m == up ? 1.f : exp2_(m - up);
+      m = up;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    }
+    const float mu = m == -kInf ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[kb][r] = exp2_(fmaf(p[kb][r], a.scale2, -mu));
+        sum += p[kb][r];
+      }
+    l += sum;
     wave_priority<1>();
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int st = 0; st < kRowSteps<T>; ++st) {
-        u32x4_t pf[NQ];
+      for (int st = 0; st < 2; ++st) {
+        const Frag<PL> pf = frag_acc<PL>(p[kb], st);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) pf[n] = frag_acc<T>(p[n][kb], st);
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t vf = frag_cols<T, DP>(cb, TILE + 32 * kb * L::RB, st, db);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) Mma<T>::run(vf, pf[n], o[n][db]);
-        }
+        for (int db = 0; db < L::DB; ++db)
+          mma<PL>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * kb * L::RB, st, db), pf, o[db]);
       }
     wave_priority<0>();
   }
 
+  l = sum32(l);
+  const int64_t row = row_index(a, it.b, head, s.q0 + iq);
+  if constexpr (SPLIT) {
+    const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
+    float* po = a.part_o + (split * all + row) * a.dim;
+    store_row<float, L::DB>(o, 1.f, reinterpret_cast<char*>(po), nullptr, a.dim, half, in);
+    if (in && half == 0) a.part_ml[split * all + row] = make_float2(m, l);
+    return;
+  }
+  const bool live = in && iq < s.nq;
+  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
+  if (!live) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const float sum = sum32(l[n]);
-    const int64_t row = row_index(a, it.b, head[n], s.q0 + iq[n]);
-    if constexpr (SPLIT) {
-      const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
-      float* po = a.part_o + (split * all + row) * a.dim;
-      store_row<float, L::DB>(o[n], 1.f, reinterpret_cast<char*>(po), nullptr, a.dim / 4, half, in[n]);
-      if (in[n] && half == 0) a.part_ml[split * all + row] = make_float2(m[n], sum);
-      continue;
-    }
-    const bool live = in[n] && iq[n] < s.nq;
-    const float inv = !live || sum == 0.f ? 0.f : 1.f / sum;
-    if (!live) {
-#pragma unroll
-      for (int db = 0; db < L::DB; ++db) o[n][db] = zero16();
-    }
-    char* orow = at_row_w(a.out, it.b, s.q0 + iq[n], head[n]);
-    char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq[n], head[n]) : nullptr;
-    store_row<T, L::DB>(o[n], inv, orow, rrow, dch, half, in[n]);
-    if (in[n] && half == 0) a.lse[row] = live && sum != 0.f ? (m[n] + __log2f(sum)) * kLn2 : -kInf;
-    if (a.max_logits) {
-      float x = live ? top[n] * a.scale : -kInf;
-      if (pack) {
-        if (half == 0 && x > -kInf) atomic_max_f32(a.max_logits + head[n], x);
-      } else {
-        x = wave_max(x);
-        if (lane == 0 && x > -kInf) atomic_max_f32(a.max_logits + head[n], x);
-      }
+    for (int db = 0; db < L::DB; ++db) o[db] = zero16();
+  }
+  char* orow = at_row_w(a.out, it.b, s.q0 + iq, head);
+  char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq, head) : nullptr;
+  store_row<T, L::DB>(o, inv, orow, rrow, a.dim, half, in);
+  if (in && half == 0) a.lse[row] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
+  if (a.max_logits) {
+    float x = live ? top * a.scale : -kInf;
+    if (pack) {
+      if (half == 0 && x > -kInf) atomic_max_f32(a.max_logits + head, x);
+    } else {
+      x = wave_max(x);
+      if (lane == 0 && x > -kInf) atomic_max_f32(a.max_logits + head, x);
     }
   }
 }
@@ -635,101 +706,66 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // ---------------------------------------------------------------------------
 // Backward.
 // ---------------------------------------------------------------------------
-// dQ: a wave holds 32 NQ queries (Q and dO rows in registers), the workgroup
+// dQ: a wave holds 32 queries (Q and dO rows in registers), the workgroup
 // passes over the keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // First it forms each row's dout . out in fp32, with what the rounding took
 // from out where the caller kept it, and writes it and log2 of the sum of
 // exponentials for k_attn_dkv: +inf where no key is visible, so that every
 // probability recomputed from it is 0.
-template <typename T, int DP, int NQ, int BN>
-__global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
-  using L = Lay<T, DP>;
-  constexpr int BM = 128 * NQ, TILE = BN * L::RB, STAGE = 2 * TILE;
+template <int PL, int DU, int BN>
+__global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
+  using L = Lay<DU>;
+  using T = typename Io<PL>::T;
+  constexpr int BM = 128, PLANE = BN * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = a.dim / L::EPC;
+  const int dch = (a.dim + 7) / 8;
   const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal);
   const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
-  const int r0 = s.tile * BM + wave * 32 * NQ;
+  const int r0 = s.tile * BM + wave * 32;
   const int t0q = s.tile * BM;
   const KeyRange wg = keys_of(a, s, t0q, min(t0q + BM, s.nq) - 1);
-  const KeyRange wv = keys_of(a, s, r0, min(r0 + 32 * NQ, s.nq) - 1);
+  const KeyRange wv = keys_of(a, s, r0, min(r0 + 32, s.nq) - 1);
   const int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
 
   const uint32_t lds0 = lds_offset(smem);
-  const uint32_t rbase = lds0 + rows_base<T, DP>(lane), cbase = lds0 + cols_base<T, DP>(lane);
-  Stager<T, DP, BN> ks, vs;
-  ks.init(static_cast<uint32_t>(a.k.token), dch);
-  vs.init(static_cast<uint32_t>(a.v.token), dch);
-  const char* const krow = at_row(a.k, it.b, s.k0, it.kvh);
-  const char* const vrow = at_row(a.v, it.b, s.k0, it.kvh);
+  const uint32_t rbase = lds0 + rows_base<DU>(lane), cbase = lds0 + cols_base<DU>(lane);
+  Stager<PL, DU, BN> ks, vs;
+  ks.init(static_cast<uint32_t>(a.sk.token), dch);
+  vs.init(static_cast<uint32_t>(a.sv.token), dch);
+  const char* const krow = at_row(a.sk, it.b, s.k0, it.kvh);
+  const char* const vrow = at_row(a.sv, it.b, s.k0, it.kvh);
   auto issue = [&](int t) __attribute__((always_inline)) {
     const uint32_t at = lds0 + (t & 1) * STAGE;
     const int64_t j = t * BN;
-    ks.issue(krow + j * a.k.token, s.nk - t * BN, dch, at, wave);
-    vs.issue(vrow + j * a.v.token, s.nk - t * BN, dch, at + TILE, wave);
+    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * BN, dch, at, wave);
+    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * BN, dch, at + TILE, wave);
   };
   if (t0 < t1) issue(t0);
 
-  u32x4_t qf[NQ][L::STEPS], df[NQ][L::STEPS];
-  float lse2[NQ], delta[NQ];
-  int jmin[NQ], jmax[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int r = r0 + 32 * n + (lane & 31), iq = min(r, s.q_rows - 1);
-    load_operand<T, DP>(at_row(a.q, it.b, s.q0 + iq, head), dch, half, qf[n]);
-    load_operand<T, DP>(at_row(a.dout, it.b, s.q0 + iq, head), dch, half, df[n]);
-    float x = 0.f;
-    {
-      u32x4_t of[L::STEPS];
-      load_operand<T, DP>(at_row(a.out, it.b, s.q0 + iq, head), dch, half, of);
-#pragma unroll
-      for (int st = 0; st < L::STEPS; ++st)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (sizeof(T) == 2) {
-            x = fmaf(__uint_as_float(df[n][st][e] << 16), __uint_as_float(of[st][e] << 16), x);
-            x = fmaf(__uint_as_float(df[n][st][e] & 0xffff0000u), __uint_as_float(of[st][e] & 0xffff0000u), x);
-          } else {
-            x = fmaf(__uint_as_float(df[n][st][e]), __uint_as_float(of[st][e]), x);
-          }
-        }
-    }
-    if constexpr (sizeof(T) == 2) {
-      if (a.res.p) {
-        u32x4_t of[L::STEPS];
-        load_operand<T, DP>(at_row(a.res, it.b, s.q0 + iq, head), dch, half, of);
-        float y = 0.f;
-#pragma unroll
-        for (int st = 0; st < L::STEPS; ++st)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y = fmaf(__uint_as_float(df[n][st][e] << 16), __uint_as_float(of[st][e] << 16), y);
-            y = fmaf(__uint_as_float(df[n][st][e] & 0xffff0000u), __uint_as_float(of[st][e] & 0xffff0000u), y);
-          }
-        x += y;
-      }
-    }
-    x = sum32(x);
-    const int64_t row = row_index(a, it.b, head, s.q0 + iq);
-    const float v = r < s.nq ? a.lse[row] : -kInf;
-    lse2[n] = v == -kInf ? kInf : v * kLog2e;
-    delta[n] = x;
-    if (half == 0 && r < s.nq) {
-      a.lse2[row] = lse2[n];
-      a.delta[row] = x;
-    }
-    jmax[n] = a.causal ? min(s.nk - 1, iq + shift) : s.nk - 1;
-    jmin[n] = a.causal && a.window ? max(0, iq + shift - a.window + 1) : 0;
+  Frag<PL> qf[L::STEPS], df[L::STEPS];
+  const int r = r0 + (lane & 31), iq = min(r, s.q_rows - 1);
+  const char* const dorow = at_row(a.dout, it.b, s.q0 + iq, head);
+  load_operand<PL, DU>(at_row(a.q, it.b, s.q0 + iq, head), a.dim, half, qf);
+  load_operand<PL, DU>(dorow, a.dim, half, df);
+  float delta = dot_rows<PL, DU>(dorow, at_row(a.out, it.b, s.q0 + iq, head), a.dim, half);
+  if (PL == 1 && a.res.p) delta += dot_rows<PL, DU>(dorow, at_row(a.res, it.b, s.q0 + iq, head), a.dim, half);
+  delta = sum32(delta);
+  const int64_t row = row_index(a, it.b, head, s.q0 + iq);
+  const float lse = r < s.nq ? a.lse[row] : -kInf;
+  const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
+  if (half == 0 && r < s.nq) {
+    a.lse2[row] = lse2;
+    a.delta[row] = delta;
   }
-  f32x16_t acc[NQ][L::DB];
+  const int jmax = a.causal ? min(s.nk - 1, iq + shift) : s.nk - 1;
+  const int jmin = a.causal && a.window ? max(0, iq + shift - a.window + 1) : 0;
+  f32x16_t acc[L::DB];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n)
-#pragma unroll
-    for (int db = 0; db < L::DB; ++db) acc[n][db] = zero16();
+  for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
   for (int t = t0; t < t1; ++t) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -739,83 +775,62 @@ __global__ __launch_bounds__(256, NQ == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
     for (int kb = 0; kb < BN / 32; ++kb) {
       const int j0 = t * BN + 32 * kb;
       if (j0 >= wv.end || j0 + 32 <= wv.beg) continue;
-      f32x16_t p[NQ], d[NQ];
+      f32x16_t p = zero16(), d = zero16();
+      wave_priority<1>();
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) p[n] = d[n] = zero16();
-      if constexpr (NQ == 1) wave_priority<1>();
+      for (int st = 0; st < L::STEPS; ++st) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * kb * L::RB, st), qf[st], p);
 #pragma unroll
-      for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t kf = frag_rows<T, DP>(rb, 32 * kb * L::RB, st);
+      for (int st = 0; st < L::STEPS; ++st) mma<PL>(frag_rows<PL, PLANE>(rb, TILE + 32 * kb * L::RB, st), df[st], d);
+      wave_priority<0>();
+      if (j0 + 32 > wv.all_end || j0 < wv.all_beg) {
+        asm volatile("; a tile that the mask cuts");
+        const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) Mma<T>::run(kf, qf[n][st], p[n]);
-      }
-#pragma unroll
-      for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t vf = frag_rows<T, DP>(rb, TILE + 32 * kb * L::RB, st);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) Mma<T>::run(vf, df[n][st], d[n]);
-      }
-      if constexpr (NQ == 1) wave_priority<0>();
-      const bool cut = j0 + 32 > wv.all_end || j0 < wv.all_beg;
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        if (cut) {
-          asm volatile("; a tile that the mask cuts");
-          const int lo = jmin[n] - j0 - 4 * half, hi = jmax[n] - j0 - 4 * half;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = 8 * (r >> 2) + (r & 3);
-            if (j < lo || j > hi) p[n][r] = -kInf;
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          d[n][r] = exp2_(fmaf(p[n][r], a.scale2, -lse2[n])) * (d[n][r] - delta[n]);
-      }
-      if constexpr (NQ == 1) wave_priority<1>();
-#pragma unroll
-      for (int st = 0; st < kRowSteps<T>; ++st) {
-        u32x4_t f[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) f[n] = frag_acc<T>(d[n], st);
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t kt = frag_cols<T, DP>(cb, 32 * kb * L::RB, st, db);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) Mma<T>::run(kt, f[n], acc[n][db]);
+        for (int e = 0; e < 16; ++e) {
+          const int j = 8 * (e >> 2) + (e & 3);
+          if (j < lo || j > hi) p[e] = -kInf;
         }
       }
-      if constexpr (NQ == 1) wave_priority<0>();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) d[e] = exp2_(fmaf(p[e], a.scale2, -lse2)) * (d[e] - delta);
+      wave_priority<1>();
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const Frag<PL> f = frag_acc<PL>(d, st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db)
+          mma<PL>(frag_cols<PL, DU, PLANE>(cb, 32 * kb * L::RB, st, db), f, acc[db]);
+      }
+      wave_priority<0>();
     }
   }
+  if (r >= s.nq) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int r = r0 + 32 * n + (lane & 31), iq = min(r, s.q_rows - 1);
-    if (r >= s.nq) {
-#pragma unroll
-      for (int db = 0; db < L::DB; ++db) acc[n][db] = zero16();
-    }
-    store_row<T, L::DB>(acc[n], a.scale, at_row_w(a.dq, it.b, s.q0 + iq, head), nullptr, dch, half, r < s.q_rows);
+    for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
   }
+  store_row<T, L::DB>(acc, a.scale, at_row_w(a.dq, it.b, s.q0 + iq, head), nullptr, a.dim, half, r < s.q_rows);
 }
 
-// dK, dV: a wave holds 32 NK keys (K rows in registers, V rows there or, VL,
-// in LDS), the workgroup passes over the queries of one head, or of all heads
+// dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in
+// LDS), the workgroup passes over the queries of one head, or of several heads
 // of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
-template <typename T, int DP, int NK, int BM, bool VL>
-__global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
-  using L = Lay<T, DP>;
-  constexpr int BK = 128 * NK, TILE = BM * L::RB, STAGE = 2 * TILE, VT = VL ? BK * L::RB : 0;
+template <int PL, int DU, int BM, bool VL>
+__global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
+  using L = Lay<DU>;
+  using T = typename Io<PL>::T;
+  constexpr int BK = 128, PLANE = BM * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
+  constexpr int VPLANE = BK * L::RB, VT = VL ? PL * VPLANE : 0;
   // V, two stages of Q and dO, two of the rows' statistics (64 floats of each kind)
   __shared__ __attribute__((aligned(1024))) char smem[VT + 2 * STAGE + 1024];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = a.dim / L::EPC;
-  const Item it = item_of(blockIdx.x, a, a.kv_split ? a.group : 1, tiles, false);
+  const int dch = (a.dim + 7) / 8;
+  const int heads = a.group / a.kv_parts;
+  const Item it = item_of(blockIdx.x, a, a.kv_parts, tiles, false);
   const Seq s = find_seq(a.seqs, it.b, it.tile, BK, true);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
-  const int k0 = s.tile * BK, w0 = k0 + wave * 32 * NK;
+  const int k0 = s.tile * BK, w0 = k0 + wave * 32;
   // queries that see a key of the workgroup
   int qb = 0, qe = s.nq;
   if (a.causal) {
@@ -824,17 +839,16 @@ __global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
   }
   if (k0 >= s.nk) qe = 0;
   const int t0 = qb / BM, per = max(0, (qe + BM - 1) / BM - t0);
-  const int heads = a.kv_split ? 1 : a.group, steps = per * heads;
-  const int h0 = it.kvh * a.group + (a.kv_split ? it.g : 0);
+  const int steps = per * heads, h0 = it.kvh * a.group + it.g * heads;
 
   const uint32_t lds0 = lds_offset(smem), stats = lds0 + VT + 2 * STAGE;
-  const uint32_t rbase = lds0 + VT + rows_base<T, DP>(lane), cbase = lds0 + VT + cols_base<T, DP>(lane);
-  const uint32_t vbase = lds0 + wave * 32 * NK * L::RB + rows_base<T, DP>(lane);
-  Stager<T, DP, BM> qs, ds;
-  qs.init(static_cast<uint32_t>(a.q.token), dch);
-  ds.init(static_cast<uint32_t>(a.dout.token), dch);
-  const char* const qrow = at_row(a.q, it.b, s.q0, h0);
-  const char* const drow = at_row(a.dout, it.b, s.q0, h0);
+  const uint32_t rbase = lds0 + VT + rows_base<DU>(lane), cbase = lds0 + VT + cols_base<DU>(lane);
+  const uint32_t vbase = lds0 + wave * 32 * L::RB + rows_base<DU>(lane);
+  Stager<PL, DU, BM> qs, ds;
+  qs.init(static_cast<uint32_t>(a.sq.token), dch);
+  ds.init(static_cast<uint32_t>(a.sdo.token), dch);
+  const char* const qrow = at_row(a.sq, it.b, s.q0, h0);
+  const char* const drow = at_row(a.sdo, it.b, s.q0, h0);
   const int64_t srow = row_index(a, it.b, h0, s.q0);
   // the next tile to load: tile nt of head h0 + nh
   int nt = t0, nh = 0;
@@ -842,8 +856,8 @@ __global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
     const uint32_t at = lds0 + VT + (i & 1) * STAGE;
     const int64_t q = nt * BM;
     const int left = s.nq - nt * BM;
-    qs.issue(qrow + nh * a.q.head + q * a.q.token, left, dch, at, wave);
-    ds.issue(drow + nh * a.dout.head + q * a.dout.token, left, dch, at + TILE, wave);
+    qs.issue(qrow + nh * a.sq.head + q * a.sq.token, a.plane, left, dch, at, wave);
+    ds.issue(drow + nh * a.sdo.head + q * a.sdo.token, a.plane, left, dch, at + TILE, wave);
     if (wave < 2) {  // the rows' statistics (queries behind the last repeat it, and are masked)
       const float* p = (wave ? a.delta : a.lse2) + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q;
       load_lds4(reinterpret_cast<const char*>(p), min(min(lane, BM - 1), left - 1) * 4, stats + (i & 1) * 512 + wave * 256);
@@ -852,31 +866,25 @@ __global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
   };
   if (steps > 0) issue(0);
 
-  u32x4_t kf[NK][L::STEPS], vf[VL ? 1 : NK][VL ? 1 : L::STEPS];
-  int qmin[NK], qmax[NK];
-#pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    const int j = min(w0 + 32 * n + (lane & 31), s.k_rows - 1);
-    load_operand<T, DP>(at_row(a.k, it.b, s.k0 + j, it.kvh), dch, half, kf[n]);
-    if constexpr (!VL) load_operand<T, DP>(at_row(a.v, it.b, s.k0 + j, it.kvh), dch, half, vf[n]);
-    qmin[n] = a.causal ? j - shift : 0;
-    qmax[n] = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
-  }
+  Frag<PL> kf[L::STEPS], vf[VL ? 1 : L::STEPS];
+  const int r = w0 + (lane & 31), j = min(r, s.k_rows - 1);
+  load_operand<PL, DU>(at_row(a.k, it.b, s.k0 + j, it.kvh), a.dim, half, kf);
+  if constexpr (!VL) load_operand<PL, DU>(at_row(a.v, it.b, s.k0 + j, it.kvh), a.dim, half, vf);
+  const int qmin = a.causal ? j - shift : 0;
+  const int qmax = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
   if constexpr (VL) {
     if (steps > 0)  // zeros beyond the head: dO's tiles repeat a chunk there
       for (int p = threadIdx.x; p < BK * L::CH; p += 256) {
-        const int r = p / L::CH, c = p % L::CH;
-        const char* row = at_row(a.v, it.b, s.k0 + min(k0 + r, s.nk - 1), it.kvh);
-        *reinterpret_cast<u32x4_t*>(smem + L::at(r, c)) =
-            c < dch ? *reinterpret_cast<const u32x4_t*>(row + c * 16) : u32x4_t{0, 0, 0, 0};
+        const int vr = p / L::CH, c = p % L::CH;
+        const Frag<PL> f = load_chunk<PL>(at_row(a.v, it.b, s.k0 + min(k0 + vr, s.nk - 1), it.kvh), c, a.dim);
+#pragma unroll
+        for (int q = 0; q < PL; ++q) *reinterpret_cast<u32x4_t*>(smem + q * VPLANE + L::at(vr, c)) = f.v[q];
       }
   }
-  f32x16_t dk[NK][L::DB], dv[NK][L::DB];
+  f32x16_t dk[L::DB], dv[L::DB];
 #pragma unroll
-  for (int n = 0; n < NK; ++n)
-#pragma unroll
-    for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = zero16();
-  const int wk_hi = min(w0 + 32 * NK, s.nk) - 1;  // the wave's last key
+  for (int db = 0; db < L::DB; ++db) dk[db] = dv[db] = zero16();
+  const int w_hi = min(w0 + 32, s.nk) - 1;  // the wave's last key
   int ct = t0;
   for (int i = 0; i < steps; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -889,105 +897,73 @@ __global__ __launch_bounds__(256, NK == 1 && sizeof(T) == 2 ? 2 : 1) void k_attn
 #pragma unroll
     for (int qk = 0; qk < BM / 32; ++qk) {
       const int q = q0 + 32 * qk;
-      if (q >= s.nq || wk_hi < w0) continue;
+      if (q >= s.nq || w_hi < w0) continue;
       if (a.causal && q + 31 + shift < w0) continue;
-      if (a.causal && a.window && q + shift - wk_hi >= a.window) continue;
-      const bool cut = q + 32 > s.nq || (a.causal && q + shift < w0 + 32 * NK - 1) ||
-                       (a.causal && a.window && q + 31 + shift - w0 >= a.window);
-      f32x16_t p[NK], d[NK];
+      if (a.causal && a.window && q + shift - w_hi >= a.window) continue;
+      f32x16_t p = zero16(), d = zero16();
+      wave_priority<1>();
 #pragma unroll
-      for (int n = 0; n < NK; ++n) p[n] = d[n] = zero16();
-      if constexpr (NK == 1) wave_priority<1>();
+      for (int st = 0; st < L::STEPS; ++st) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * qk * L::RB, st), kf[st], p);
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t f = frag_rows<T, DP>(rb, 32 * qk * L::RB, st);
-#pragma unroll
-        for (int n = 0; n < NK; ++n) Mma<T>::run(f, kf[n][st], p[n]);
+        const Frag<PL> f = frag_rows<PL, PLANE>(rb, TILE + 32 * qk * L::RB, st);
+        if constexpr (VL) mma<PL>(f, frag_rows<PL, VPLANE>(vbase, 0, st), d);
+        else mma<PL>(f, vf[st], d);
       }
-#pragma unroll
-      for (int st = 0; st < L::STEPS; ++st) {
-        const u32x4_t f = frag_rows<T, DP>(rb, TILE + 32 * qk * L::RB, st);
-#pragma unroll
-        for (int n = 0; n < NK; ++n) {
-          if constexpr (VL) Mma<T>::run(f, frag_rows<T, DP>(vbase, 32 * n * L::RB, st), d[n]);
-          else Mma<T>::run(f, vf[n][st], d[n]);
-        }
-      }
-      if constexpr (NK == 1) wave_priority<0>();
-      if (cut) {
+      wave_priority<0>();
+      if (q + 32 > s.nq || (a.causal && q + shift < w0 + 31) ||
+          (a.causal && a.window && q + 31 + shift - w0 >= a.window)) {
         asm volatile("; a tile that the mask cuts");
+        const int lo = qmin - q - 4 * half, hi = qmax - q - 4 * half;
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-          const int lo = qmin[n] - q - 4 * half, hi = qmax[n] - q - 4 * half;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int i = 8 * (r >> 2) + (r & 3);
-            if (i < lo || i > hi) p[n][r] = -kInf;
-          }
+        for (int e = 0; e < 16; ++e) {
+          const int x = 8 * (e >> 2) + (e & 3);
+          if (x < lo || x > hi) p[e] = -kInf;
         }
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const u32x4_t ls = lds16(sb + (32 * qk + 8 * g) * 4), de = lds16(sb + 256 + (32 * qk + 8 * g) * 4);
 #pragma unroll
-        for (int n = 0; n < NK; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = exp2_(fmaf(p[n][4 * g + e], a.scale2, -__uint_as_float(ls[e])));
-            p[n][4 * g + e] = x;
-            d[n][4 * g + e] = x * (d[n][4 * g + e] - __uint_as_float(de[e]));
-          }
-      }
-      if constexpr (NK == 1) wave_priority<1>();
-#pragma unroll
-      for (int st = 0; st < kRowSteps<T>; ++st) {
-        u32x4_t f[NK];
-#pragma unroll
-        for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(p[n], st);
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t x = frag_cols<T, DP>(cb, TILE + 32 * qk * L::RB, st, db);
-#pragma unroll
-          for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dv[n][db]);
+        for (int e = 0; e < 4; ++e) {
+          const float x = exp2_(fmaf(p[4 * g + e], a.scale2, -__uint_as_float(ls[e])));
+          p[4 * g + e] = x;
+          d[4 * g + e] = x * (d[4 * g + e] - __uint_as_float(de[e]));
         }
       }
+      wave_priority<1>();
 #pragma unroll
-      for (int st = 0; st < kRowSteps<T>; ++st) {
-        u32x4_t f[NK];
+      for (int st = 0; st < 2; ++st) {
+        const Frag<PL> f = frag_acc<PL>(p, st);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) f[n] = frag_acc<T>(d[n], st);
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db) {
-          const u32x4_t x = frag_cols<T, DP>(cb, 32 * qk * L::RB, st, db);
-#pragma unroll
-          for (int n = 0; n < NK; ++n) Mma<T>::run(x, f[n], dk[n][db]);
-        }
+        for (int db = 0; db < L::DB; ++db)
+          mma<PL>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * qk * L::RB, st, db), f, dv[db]);
       }
-      if constexpr (NK == 1) wave_priority<0>();
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const Frag<PL> f = frag_acc<PL>(d, st);
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) mma<PL>(frag_cols<PL, DU, PLANE>(cb, 32 * qk * L::RB, st, db), f, dk[db]);
+      }
+      wave_priority<0>();
     }
   }
+  if (r >= s.nk) {
 #pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    const int r = w0 + 32 * n + (lane & 31), j = min(r, s.k_rows - 1);
-    if (r >= s.nk) {
-#pragma unroll
-      for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = zero16();
-    }
-    const bool on = r < s.k_rows;
-    if (a.kv_split) {
-      const int64_t row = (static_cast<int64_t>(it.b) * a.seqs.k_tokens + s.k0 + j) * a.q_heads + h0;
-      store_row<float, L::DB>(dk[n], a.scale, reinterpret_cast<char*>(a.part_dk + row * a.dim), nullptr, a.dim / 4,
-                              half, on);
-      store_row<float, L::DB>(dv[n], 1.f, reinterpret_cast<char*>(a.part_dv + row * a.dim), nullptr, a.dim / 4,
-                              half, on);
-    } else {
-      store_row<T, L::DB>(dk[n], a.scale, at_row_w(a.dk, it.b, s.k0 + j, it.kvh), nullptr, dch, half, on);
-      store_row<T, L::DB>(dv[n], 1.f, at_row_w(a.dv, it.b, s.k0 + j, it.kvh), nullptr, dch, half, on);
-    }
+    for (int db = 0; db < L::DB; ++db) dk[db] = dv[db] = zero16();
+  }
+  const bool on = r < s.k_rows;
+  if (a.kv_parts > 1) {
+    const int64_t row = ((static_cast<int64_t>(it.b) * a.seqs.k_tokens + s.k0 + j) * a.kv_heads + it.kvh) * a.kv_parts + it.g;
+    store_row<float, L::DB>(dk, a.scale, reinterpret_cast<char*>(a.part_dk + row * a.dim), nullptr, a.dim, half, on);
+    store_row<float, L::DB>(dv, 1.f, reinterpret_cast<char*>(a.part_dv + row * a.dim), nullptr, a.dim, half, on);
+  } else {
+    store_row<T, L::DB>(dk, a.scale, at_row_w(a.dk, it.b, s.k0 + j, it.kvh), nullptr, a.dim, half, on);
+    store_row<T, L::DB>(dv, 1.f, at_row_w(a.dv, it.b, s.k0 + j, it.kvh), nullptr, a.dim, half, on);
   }
 }
 
-// Sums the heads of each group, in order: a thread has 4 elements of dk or dv.
+// Sums the parts of each group, in order: a thread has 4 elements of dk or dv.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
   const int quads = a.dim / 4;
@@ -1003,9 +979,9 @@ __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
   if (a.seqs.q_off) {  // rows behind the last sequence stay as they are
     if (j < a.seqs.k_off[0] || j >= a.seqs.k_off[a.seqs.n_seq]) return;
   }
-  const float* p = (second ? a.part_dv : a.part_dk) + (tok * a.q_heads + static_cast<int64_t>(head) * a.group) * a.dim + 4 * quad;
+  const float* p = (second ? a.part_dv : a.part_dk) + (tok * a.kv_heads + head) * a.kv_parts * a.dim + 4 * quad;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int g = 0; g < a.group; ++g, p += a.dim) {
+  for (int g = 0; g < a.kv_parts; ++g, p += a.dim) {
     const float4 y = *reinterpret_cast<const float4*>(p);
     x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
   }
@@ -1204,44 +1180,74 @@ bool packs_heads(const Seqs& s, int group) {
   return !s.q_off && group > 1 && int64_t(s.q_tokens) * group <= 128;
 }
 
-template <typename T, int DP, int NQ, int BN>
-hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
-  const bool pack = packs_heads(a.seqs, a.group);
-  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128 * NQ);
-  const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
-  const dim3 g(static_cast<unsigned>(grid)), b(256);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, NQ, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
-  else hipLaunchKernelGGL((k_attn_fwd<T, DP, NQ, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
-  hipLaunchKernelGGL((k_attn_join<T>), dim3(static_cast<unsigned>(rows)), b, 0, st, a);
+// The arrays that the tiles of a pass come from: the caller's, or (fp32) the
+// planes, which this launches the making of.
+hipError_t stage_sources(AttnArgs& a, int dtype, bool backward, hipStream_t st) {
+  a.sq = a.q; a.sk = a.k; a.sv = a.v; a.sdo = a.dout;
+  a.plane = 0;
+  if (dtype == DT_BF16) return hipSuccess;
+  const int chunks = (a.dim + 7) / 8;
+  a.plane = chunks * 16;
+  SplitArgs x{};
+  x.dim = a.dim;
+  const auto add = [&](const Heads& from, char* to, int tokens, int heads, Heads& staged) {
+    x.from[x.n] = from;
+    x.to[x.n] = to;
+    x.tokens[x.n] = tokens;
+    x.heads[x.n] = heads;
+    x.first[x.n + 1] = x.first[x.n] + a.seqs.batch * tokens * heads * chunks;
+    ++x.n;
+    staged = Heads{to, int64_t(heads) * tokens * 3 * a.plane, int64_t(3) * a.plane, int64_t(tokens) * 3 * a.plane};
+  };
+  add(a.k, a.split_k, a.seqs.k_tokens, a.kv_heads, a.sk);
+  add(a.v, a.split_v, a.seqs.k_tokens, a.kv_heads, a.sv);
+  if (backward) {
+    add(a.q, a.split_q, a.seqs.q_tokens, a.q_heads, a.sq);
+    add(a.dout, a.split_do, a.seqs.q_tokens, a.q_heads, a.sdo);
+  }
+  if (x.first[x.n] == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_split, dim3(static_cast<unsigned>((x.first[x.n] + 255) / 256)), dim3(256), 0, st, x);
   return hipGetLastError();
 }
 
-template <typename T, int DP, int NQ, int NK, int TQ, int TK, bool VL>
+template <int PL, int DU, int BN>
+hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
+  const bool pack = packs_heads(a.seqs, a.group);
+  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128);
+  const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
+  const dim3 g(static_cast<unsigned>(grid)), b(256);
+  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
+  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
+  hipLaunchKernelGGL((k_attn_join<typename Io<PL>::T>), dim3(static_cast<unsigned>(rows)), b, 0, st, a);
+  return hipGetLastError();
+}
+
+template <int PL, int DU, int BN, int BM, bool VL>
 hipError_t backward_of(const AttnArgs& a, hipStream_t st) {
   const dim3 b(256);
   hipError_t e;
   if (a.seqs.q_tokens > 0) {
-    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 * NQ);
-    hipLaunchKernelGGL((k_attn_dq<T, DP, NQ, TQ>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
+    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128);
+    hipLaunchKernelGGL((k_attn_dq<PL, DU, BN>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
                        st, a, int(tiles));
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.seqs.k_tokens == 0) return hipSuccess;
-  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 * NK);
-  const int64_t grid = a.seqs.batch * a.kv_heads * (a.kv_split ? a.group : 1) * tiles;
-  hipLaunchKernelGGL((k_attn_dkv<T, DP, NK, TK, VL>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
-  if ((e = hipGetLastError()) != hipSuccess || !a.kv_split) return e;
+  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128);
+  const int64_t grid = a.seqs.batch * a.kv_heads * a.kv_parts * tiles;
+  hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, VL>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
+  if ((e = hipGetLastError()) != hipSuccess || a.kv_parts == 1) return e;
   const int64_t n = 2 * a.seqs.batch * int64_t(a.seqs.k_tokens) * a.kv_heads * (a.dim / 4);
-  hipLaunchKernelGGL((k_attn_sum_heads<T>), dim3(static_cast<unsigned>((n + 255) / 256)), b, 0, st, a);
+  hipLaunchKernelGGL((k_attn_sum_heads<typename Io<PL>::T>), dim3(static_cast<unsigned>((n + 255) / 256)), b, 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype, bool causal, int window) {
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window) {
   if (s.q_off || (causal && window)) return 1;
   const bool pack = packs_heads(s, q_heads / kv_heads);
   const int64_t items = s.batch * (pack ? int64_t(kv_heads) : q_heads * tiles_of(s, s.q_tokens, 128));
@@ -1251,21 +1257,26 @@ int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype,
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
 }
 
-bool backward_splits_heads(const Seqs& s, int q_heads, int kv_heads, int dim, int dtype) {
-  return q_heads != kv_heads;
+int backward_parts(const Seqs& s, int q_heads, int kv_heads) {
+  const int group = q_heads / kv_heads;
+  const int64_t items = s.batch * kv_heads * tiles_of(s, s.k_tokens, 128);
+  for (int p = 1; p < group; ++p)
+    if (group % p == 0 && items * p >= 1024) return p;
+  return group;
 }
 
-hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+hipError_t run_attention_forward(AttnArgs a, int dtype, hipStream_t st, LaunchTimer* timer) {
   if (a.seqs.batch * a.seqs.q_tokens == 0) return hipSuccess;
   Timed tm(timer, KK_ATTENTION_FWD, st);
-  hipError_t e;
+  hipError_t e = stage_sources(a, dtype, false, st);
+  if (e != hipSuccess) return e;
   const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
   if (dtype == DT_BF16)
-    e = pick([&] { return forward_of<uint16_t, 64, 1, 64>(a, st); }, [&] { return forward_of<uint16_t, 96, 1, 64>(a, st); },
-             [&] { return forward_of<uint16_t, 128, 1, 64>(a, st); });
+    e = pick([&] { return forward_of<1, 64, 64>(a, st); }, [&] { return forward_of<1, 96, 64>(a, st); },
+             [&] { return forward_of<1, 128, 64>(a, st); });
   else
-    e = pick([&] { return forward_of<float, 64, 1, 64>(a, st); }, [&] { return forward_of<float, 96, 1, 32>(a, st); },
-             [&] { return forward_of<float, 128, 1, 32>(a, st); });
+    e = pick([&] { return forward_of<3, 64, 32>(a, st); }, [&] { return forward_of<3, 96, 32>(a, st); },
+             [&] { return forward_of<3, 128, 32>(a, st); });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(4.0 * pairs_of(a) * a.dim, 0,
@@ -1273,18 +1284,19 @@ hipError_t run_attention_forward(const AttnArgs& a, int dtype, hipStream_t st, L
   return e;
 }
 
-hipError_t run_attention_backward(const AttnArgs& a, int dtype, hipStream_t st, LaunchTimer* timer) {
+hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchTimer* timer) {
   if (a.seqs.batch == 0) return hipSuccess;
   Timed tm(timer, KK_ATTENTION_BWD, st);
-  hipError_t e;
+  hipError_t e = stage_sources(a, dtype, true, st);
+  if (e != hipSuccess) return e;
   const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
   if (dtype == DT_BF16)
-    e = pick([&] { return backward_of<uint16_t, 64, 1, 1, 64, 32, false>(a, st); },
-             [&] { return backward_of<uint16_t, 96, 1, 1, 64, 32, true>(a, st); }, [&] { return backward_of<uint16_t, 128, 1, 1, 64, 32, true>(a, st); });
+    e = pick([&] { return backward_of<1, 64, 64, 32, false>(a, st); },
+             [&] { return backward_of<1, 96, 64, 32, true>(a, st); }, [&] { return backward_of<1, 128, 64, 32, true>(a, st); });
   else
-    e = pick([&] { return backward_of<float, 64, 1, 1, 32, 32, false>(a, st); },
-             [&] { return backward_of<float, 96, 1, 1, 32, 32, true>(a, st); },
-             [&] { return backward_of<float, 128, 1, 1, 32, 32, true>(a, st); });
+    e = pick([&] { return backward_of<3, 64, 32, 32, false>(a, st); },
+             [&] { return backward_of<3, 96, 32, 32, false>(a, st); },
+             [&] { return backward_of<3, 128, 32, 32, false>(a, st); });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(10.0 * pairs_of(a) * a.dim, 0,
