@@ -492,20 +492,23 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 }
 
 // ---------------------------------------------------------------------------
-// Forward.  A workgroup of 4 waves holds 128 queries (32 a wave) and passes
-// over the keys in tiles of BN, double-buffered in LDS, keeping the running
-// maximum and sum.
+// Forward.  A wave holds 32 queries and passes over the keys in tiles of BN,
+// staged in LDS (NST stages), keeping the running maximum and sum.  WS = 1: the
+// workgroup's 4 waves hold 128 queries and share each tile.  WS > 1: WS waves
+// share their queries and take every WS-th tile, and are joined at the end; for
+// requests with too few rows to fill the device.
 // ---------------------------------------------------------------------------
-template <int PL, int DU, int BN, bool SPLIT>
-__global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
+template <int PL, int DU, int BN, int WS, int NST, bool SPLIT>
+__global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
   constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
-  constexpr int BM = 128, KB = BN / 32, PLANE = BN * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  constexpr int BM = 128 / WS, KB = BN / 32, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
+  constexpr int JOIN = (WS - 1) * (4 / WS) * (L::DB * 16 + 3) * 256;
+  __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE > JOIN ? NST * STAGE : JOIN];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = (a.dim + 7) / 8;
+  const int ws = wave % WS, dch = (a.dim + 7) / 8;
   int bid = blockIdx.x, split = 0;
   if constexpr (SPLIT) {
     const int items = gridDim.x / a.splits;
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(A
 
   // the lane's rows.  pack: the rows are all heads of the group, each with all queries
   const int rows = pack ? s.q_rows * a.group : s.q_rows;
-  const int r0 = s.tile * BM + wave * 32;
+  const int r0 = s.tile * BM + wave / WS * 32;
   const int r = r0 + (lane & 31);
   const bool in = r < rows;
   int iq = min(r, rows - 1), g = it.g;
@@ -535,7 +538,7 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(A
   const int last = min(s.q_rows, s.nq) - 1;
   const KeyRange wg = pack ? keys_of(a, s, 0, last) : keys_of(a, s, s.tile * BM, min(s.tile * BM + BM - 1, last));
   const KeyRange wv = r0 >= rows ? KeyRange{0, 0, 0, 0} : pack ? wg : keys_of(a, s, r0, min(r0 + 31, last));
-  int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
+  int t0 = wg.beg / SR, t1 = (wg.end + SR - 1) / SR;
   if constexpr (SPLIT) {
     const int per = (max(t1 - t0, 0) + a.splits - 1) / a.splits;
     t0 += split * per;
@@ -543,33 +546,37 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(A
   }
 
   const uint32_t lds0 = lds_offset(smem);
-  const uint32_t rbase = lds0 + rows_base<DU>(lane), cbase = lds0 + cols_base<DU>(lane);
-  Stager<PL, DU, BN> ks, vs;
+  const uint32_t own = lds0 + ws * BN * L::RB, rbase = own + rows_base<DU>(lane), cbase = own + cols_base<DU>(lane);
+  Stager<PL, DU, SR> ks, vs;
   ks.init(static_cast<uint32_t>(a.sk.token), dch);
   vs.init(static_cast<uint32_t>(a.sv.token), dch);
   const char* const krow = at_row(a.sk, it.b, s.k0, it.kvh);
   const char* const vrow = at_row(a.sv, it.b, s.k0, it.kvh);
   auto issue = [&](int t) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + (t & 1) * STAGE;
-    const int64_t j = t * BN;
-    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * BN, dch, at, wave);
-    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * BN, dch, at + TILE, wave);
+    const uint32_t at = lds0 + t % NST * STAGE;
+    const int64_t j = t * SR;
+    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * SR, dch, at, wave);
+    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * SR, dch, at + TILE, wave);
   };
 
   f32x16_t o[L::DB];
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) o[db] = zero16();
   float m = -kInf, l = 0.f, top = -kInf;
-  if (t0 < t1) issue(t0);
+  if (NST > 1 && t0 < t1) issue(t0);
   Frag<PL> qf[L::STEPS];
   load_operand<PL, DU>(at_row(a.q, it.b, s.q0 + iq, head), a.dim, half, qf);
   for (int t = t0; t < t1; ++t) {
+    if constexpr (NST == 1) {
+      __syncthreads();
+      issue(t);
+    }
     wait_loads();
     __syncthreads();  // tile t has landed, and every wave is done with tile t - 1
-    if (t + 1 < t1) issue(t + 1);
-    const int j0 = t * BN;
+    if (NST > 1 && t + 1 < t1) issue(t + 1);
+    const int j0 = t * SR + ws * BN;
     if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
-    const uint32_t rb = rbase + (t & 1) * STAGE, cb = cbase + (t & 1) * STAGE;
+    const uint32_t rb = rbase + t % NST * STAGE, cb = cbase + t % NST * STAGE;
     f32x16_t p[KB];
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -637,6 +644,43 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_fwd(A
   }
 
   l = sum32(l);
+  if constexpr (WS > 1) {  // the waves that shared the queries, in order
+    float* const at = reinterpret_cast<float*>(smem) + wave / WS * (WS - 1) * (L::DB * 16 + 3) * 64 + lane;
+    __syncthreads();
+    if (ws > 0) {
+      float* const x = at + (ws - 1) * (L::DB * 16 + 3) * 64;
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[(db * 16 + e) * 64] = o[db][e];
+      x[L::DB * 16 * 64] = m;
+      x[(L::DB * 16 + 1) * 64] = l;
+      x[(L::DB * 16 + 2) * 64] = top;
+    }
+    __syncthreads();
+    if (ws > 0) return;
+    float all = m;
+#pragma unroll
+    for (int w = 0; w < WS - 1; ++w) all = fmaxf(all, at[(w * (L::DB * 16 + 3) + L::DB * 16) * 64]);
+    const float f = m == -kInf ? 0.f : exp2_(m - all);
+    m = all;
+    l *= f;
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] *= f;
+#pragma unroll
+    for (int w = 0; w < WS - 1; ++w) {
+      const float* const x = at + w * (L::DB * 16 + 3) * 64;
+      const float mw = x[L::DB * 16 * 64], fw = mw == -kInf ? 0.f : exp2_(mw - all);
+      l = fmaf(x[(L::DB * 16 + 1) * 64], fw, l);
+      top = fmaxf(top, x[(L::DB * 16 + 2) * 64]);
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] = fmaf(x[(db * 16 + e) * 64], fw, o[db][e]);
+    }
+  }
   const int64_t row = row_index(a, it.b, head, s.q0 + iq);
   if constexpr (SPLIT) {
     const int64_t all = static_cast<int64_t>(a.seqs.batch) * a.q_heads * a.seqs.q_tokens;
@@ -735,46 +779,72 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // ---------------------------------------------------------------------------
 // Backward.
 // ---------------------------------------------------------------------------
+// Sums the accumulators of the WS waves that share their rows, in order, into
+// the first of them, through LDS that nothing else is read from any more; true
+// in that wave.
+template <int WS, int DB>
+__device__ __forceinline__ bool join_waves(f32x16_t* acc, char* smem, int wave, int lane) {
+  const int ws = wave % WS;
+  float* const at = reinterpret_cast<float*>(smem) + wave / WS * (WS - 1) * DB * 1024 + lane;
+  __syncthreads();
+  if (ws > 0) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) at[((ws - 1) * DB * 16 + db * 16 + e) * 64] = acc[db][e];
+  }
+  __syncthreads();
+  if (ws > 0) return false;
+#pragma unroll
+  for (int w = 0; w < WS - 1; ++w)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[db][e] += at[(w * DB * 16 + db * 16 + e) * 64];
+  return true;
+}
+
 // dQ: a wave holds 32 queries (Q and dO rows in registers), the workgroup
 // passes over the keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // First it forms each row's dout . out in fp32, with what the rounding took
 // from out where the caller kept it, and writes it and log2 of the sum of
 // exponentials for k_attn_dkv: +inf where no key is visible, so that every
 // probability recomputed from it is 0.
-template <int PL, int DU, int BN>
-__global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
+template <int PL, int DU, int BN, int WS, int NST>
+__global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
   constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
-  constexpr int BM = 128, PLANE = BN * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  constexpr int BM = 128 / WS, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
+  constexpr int JOIN = (WS - 1) * (4 / WS) * L::DB * 4096;
+  __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE > JOIN ? NST * STAGE : JOIN];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = (a.dim + 7) / 8;
+  const int ws = wave % WS, dch = (a.dim + 7) / 8;
   const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal);
   const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
-  const int r0 = s.tile * BM + wave * 32;
+  const int r0 = s.tile * BM + wave / WS * 32;
   const int t0q = s.tile * BM;
   const KeyRange wg = keys_of(a, s, t0q, min(t0q + BM, s.nq) - 1);
   const KeyRange wv = keys_of(a, s, r0, min(r0 + 32, s.nq) - 1);
-  const int t0 = wg.beg / BN, t1 = (wg.end + BN - 1) / BN;
+  const int t0 = wg.beg / SR, t1 = (wg.end + SR - 1) / SR;
 
   const uint32_t lds0 = lds_offset(smem);
-  const uint32_t rbase = lds0 + rows_base<DU>(lane), cbase = lds0 + cols_base<DU>(lane);
-  Stager<PL, DU, BN> ks, vs;
+  const uint32_t own = lds0 + ws * BN * L::RB, rbase = own + rows_base<DU>(lane), cbase = own + cols_base<DU>(lane);
+  Stager<PL, DU, SR> ks, vs;
   ks.init(static_cast<uint32_t>(a.sk.token), dch);
   vs.init(static_cast<uint32_t>(a.sv.token), dch);
   const char* const krow = at_row(a.sk, it.b, s.k0, it.kvh);
   const char* const vrow = at_row(a.sv, it.b, s.k0, it.kvh);
   auto issue = [&](int t) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + (t & 1) * STAGE;
-    const int64_t j = t * BN;
-    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * BN, dch, at, wave);
-    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * BN, dch, at + TILE, wave);
+    const uint32_t at = lds0 + t % NST * STAGE;
+    const int64_t j = t * SR;
+    ks.issue(krow + j * a.sk.token, a.plane, s.nk - t * SR, dch, at, wave);
+    vs.issue(vrow + j * a.sv.token, a.plane, s.nk - t * SR, dch, at + TILE, wave);
   };
-  if (t0 < t1) issue(t0);
+  if (NST > 1 && t0 < t1) issue(t0);
 
   Frag<PL> qf[L::STEPS], df[L::STEPS];
   const int r = r0 + (lane & 31), iq = min(r, s.q_rows - 1);
@@ -787,7 +857,7 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(At
   const int64_t row = row_index(a, it.b, head, s.q0 + iq);
   const float lse = r < s.nq ? a.lse[row] : -kInf;
   const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
-  if (half == 0 && r < s.nq) {
+  if (ws == 0 && half == 0 && r < s.nq) {
     a.lse2[row] = lse2;
     a.delta[row] = delta;
   }
@@ -797,13 +867,17 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(At
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
   for (int t = t0; t < t1; ++t) {
+    if constexpr (NST == 1) {
+      __syncthreads();
+      issue(t);
+    }
     wait_loads();
     __syncthreads();
-    if (t + 1 < t1) issue(t + 1);
-    const uint32_t rb = rbase + (t & 1) * STAGE, cb = cbase + (t & 1) * STAGE;
+    if (NST > 1 && t + 1 < t1) issue(t + 1);
+    const uint32_t rb = rbase + t % NST * STAGE, cb = cbase + t % NST * STAGE;
 #pragma unroll
     for (int kb = 0; kb < BN / 32; ++kb) {
-      const int j0 = t * BN + 32 * kb;
+      const int j0 = t * SR + ws * BN + 32 * kb;
       if (j0 >= wv.end || j0 + 32 <= wv.beg) continue;
       f32x16_t p = zero16(), d = zero16();
       wave_priority<PL == 1>();
@@ -836,6 +910,9 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(At
       wave_priority<0>();
     }
   }
+  if constexpr (WS > 1) {
+    if (!join_waves<WS, L::DB>(acc, smem, wave, lane)) return;
+  }
   if (r >= s.nq) {
 #pragma unroll
     for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
@@ -846,24 +923,27 @@ __global__ __launch_bounds__(256, PL == 1 || DU <= 64 ? 2 : 1) void k_attn_dq(At
 // dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in
 // LDS), the workgroup passes over the queries of one head, or of several heads
 // of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
-template <int PL, int DU, int BM, bool VL>
-__global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
+template <int PL, int DU, int BM, int WS, int NST, bool VL>
+__global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
   constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
-  constexpr int BK = 128, PLANE = BM * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
+  constexpr int BK = 128 / WS, SR = BM * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
   constexpr int VPLANE = BK * L::RB, VT = VL ? PL * VPLANE : 0;
-  // V, two stages of Q and dO, two of the rows' statistics (64 floats of each kind)
-  __shared__ __attribute__((aligned(1024))) char smem[VT + 2 * STAGE + 1024];
+  constexpr int JOIN = (WS - 1) * (4 / WS) * L::DB * 4096;
+  static_assert(SR <= 128, "the rows' statistics");
+  // V, the stages of Q and dO, those of the rows' statistics (128 floats of each kind)
+  constexpr int USED = VT + NST * (STAGE + 1024);
+  __shared__ __attribute__((aligned(1024))) char smem[USED > JOIN ? USED : JOIN];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dch = (a.dim + 7) / 8;
+  const int ws = wave % WS, dch = (a.dim + 7) / 8;
   const int heads = a.group / a.kv_parts;
   const Item it = item_of(blockIdx.x, a, a.kv_parts, tiles, false);
   const Seq s = find_seq(a.seqs, it.b, it.tile, BK, true);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
-  const int k0 = s.tile * BK, w0 = k0 + wave * 32;
+  const int k0 = s.tile * BK, w0 = k0 + wave / WS * 32;
   // queries that see a key of the workgroup
   int qb = 0, qe = s.nq;
   if (a.causal) {
@@ -871,13 +951,13 @@ __global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, i
     if (a.window) qe = min(qe, min(k0 + BK, s.nk) - 1 - shift + a.window);
   }
   if (k0 >= s.nk) qe = 0;
-  const int t0 = qb / BM, per = max(0, (qe + BM - 1) / BM - t0);
+  const int t0 = qb / SR, per = max(0, (qe + SR - 1) / SR - t0);
   const int steps = per * heads, h0 = it.kvh * a.group + it.g * heads;
 
-  const uint32_t lds0 = lds_offset(smem), stats = lds0 + VT + 2 * STAGE;
-  const uint32_t rbase = lds0 + VT + rows_base<DU>(lane), cbase = lds0 + VT + cols_base<DU>(lane);
-  const uint32_t vbase = lds0 + wave * 32 * L::RB + rows_base<DU>(lane);
-  Stager<PL, DU, BM> qs, ds;
+  const uint32_t lds0 = lds_offset(smem), stats = lds0 + VT + NST * STAGE;
+  const uint32_t own = lds0 + VT + ws * BM * L::RB, rbase = own + rows_base<DU>(lane), cbase = own + cols_base<DU>(lane);
+  const uint32_t vbase = lds0 + wave / WS * 32 * L::RB + rows_base<DU>(lane);
+  Stager<PL, DU, SR> qs, ds;
   qs.init(static_cast<uint32_t>(a.sq.token), dch);
   ds.init(static_cast<uint32_t>(a.sdo.token), dch);
   const char* const qrow = at_row(a.sq, it.b, s.q0, h0);
@@ -886,18 +966,20 @@ __global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, i
   // the next tile to load: tile nt of head h0 + nh
   int nt = t0, nh = 0;
   auto issue = [&](int i) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + VT + (i & 1) * STAGE;
-    const int64_t q = nt * BM;
-    const int left = s.nq - nt * BM;
+    const uint32_t at = lds0 + VT + i % NST * STAGE;
+    const int64_t q = nt * SR;
+    const int left = s.nq - nt * SR;
     qs.issue(qrow + nh * a.sq.head + q * a.sq.token, a.plane, left, dch, at, wave);
     ds.issue(drow + nh * a.sdo.head + q * a.sdo.token, a.plane, left, dch, at + TILE, wave);
-    if (wave < 2) {  // the rows' statistics (queries behind the last repeat it, and are masked)
-      const float* p = (wave ? a.delta : a.lse2) + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q;
-      load_lds4(reinterpret_cast<const char*>(p), min(min(lane, BM - 1), left - 1) * 4, stats + (i & 1) * 512 + wave * 256);
+    // the rows' statistics, 64 a wave (queries behind the last repeat it, and are masked)
+    if (wave < 2 || SR > 64) {
+      const float* p = (wave & 1 ? a.delta : a.lse2) + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q;
+      load_lds4(reinterpret_cast<const char*>(p), min(min((wave >> 1) * 64 + lane, SR - 1), left - 1) * 4,
+                stats + i % NST * 1024 + (wave & 1) * 512 + (wave >> 1) * 256);
     }
     if (++nt == t0 + per) { nt = t0; ++nh; }
   };
-  if (steps > 0) issue(0);
+  if (NST > 1 && steps > 0) issue(0);
 
   Frag<PL> kf[L::STEPS], vf[VL ? 1 : L::STEPS];
   const int r = w0 + (lane & 31), j = min(r, s.k_rows - 1);
@@ -920,12 +1002,16 @@ __global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, i
   const int w_hi = min(w0 + 32, s.nk) - 1;  // the wave's last key
   int ct = t0;
   for (int i = 0; i < steps; ++i) {
+    if constexpr (NST == 1) {
+      __syncthreads();
+      issue(i);
+    }
     wait_loads();
     __syncthreads();
-    if (i + 1 < steps) issue(i + 1);
-    const uint32_t rb = rbase + (i & 1) * STAGE, cb = cbase + (i & 1) * STAGE;
-    const uint32_t sb = stats + (i & 1) * 512 + 16 * half;
-    const int q0 = ct * BM;
+    if (NST > 1 && i + 1 < steps) issue(i + 1);
+    const uint32_t rb = rbase + i % NST * STAGE, cb = cbase + i % NST * STAGE;
+    const uint32_t sb = stats + i % NST * 1024 + ws * BM * 4 + 16 * half;
+    const int q0 = ct * SR + ws * BM;
     if (++ct == t0 + per) ct = t0;
 #pragma unroll
     for (int qk = 0; qk < BM / 32; ++qk) {
@@ -957,7 +1043,7 @@ __global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, i
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const u32x4_t ls = lds16(sb + (32 * qk + 8 * g) * 4), de = lds16(sb + 256 + (32 * qk + 8 * g) * 4);
+        const u32x4_t ls = lds16(sb + (32 * qk + 8 * g) * 4), de = lds16(sb + 512 + (32 * qk + 8 * g) * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x = exp2_(fmaf(p[4 * g + e], a.scale2, -__uint_as_float(ls[e])));
@@ -982,6 +1068,10 @@ __global__ __launch_bounds__(256, PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, i
       interleave<PR * 4 * L::DB, PL * 8 * L::DB, 6>();
       wave_priority<0>();
     }
+  }
+  if constexpr (WS > 1) {
+    join_waves<WS, L::DB>(dk, smem, wave, lane);
+    if (!join_waves<WS, L::DB>(dv, smem, wave, lane)) return;
   }
   if (r >= s.nk) {
 #pragma unroll
@@ -1245,14 +1335,14 @@ hipError_t stage_sources(AttnArgs& a, int dtype, bool backward, hipStream_t st) 
   return hipGetLastError();
 }
 
-template <int PL, int DU, int BN>
+template <int PL, int DU, int BN, int WS, int NST>
 hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   const bool pack = packs_heads(a.seqs, a.group);
-  const int64_t tiles = pack ? 1 : tiles_of(a.seqs, a.seqs.q_tokens, 128);
+  const int64_t tiles = tiles_of(a.seqs, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 128 / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
   const dim3 g(static_cast<unsigned>(grid)), b(256);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, true>), g, b, 0, st, a, int(tiles), int(pack));
-  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, false>), g, b, 0, st, a, int(tiles), int(pack));
+  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, true>), g, b, 0, st, a, int(tiles), int(pack));
+  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, false>), g, b, 0, st, a, int(tiles), int(pack));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
@@ -1260,30 +1350,58 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int PL, int DU, int BN, int BM, bool VL>
-hipError_t backward_of(const AttnArgs& a, hipStream_t st) {
-  const dim3 b(256);
-  hipError_t e;
-  if (a.seqs.q_tokens > 0) {
-    const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128);
-    hipLaunchKernelGGL((k_attn_dq<PL, DU, BN>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)), b, 0,
-                       st, a, int(tiles));
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.seqs.k_tokens == 0) return hipSuccess;
-  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128);
-  const int64_t grid = a.seqs.batch * a.kv_heads * a.kv_parts * tiles;
-  hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, VL>), dim3(static_cast<unsigned>(grid)), b, 0, st, a, int(tiles));
-  if ((e = hipGetLastError()) != hipSuccess || a.kv_parts == 1) return e;
-  const int64_t n = 2 * a.seqs.batch * int64_t(a.seqs.k_tokens) * a.kv_heads * (a.dim / 4);
-  hipLaunchKernelGGL((k_attn_sum_heads<typename Io<PL>::T>), dim3(static_cast<unsigned>((n + 255) / 256)), b, 0, st, a);
+template <int PL, int DU, int BN, int WS, int NST>
+hipError_t dq_of(const AttnArgs& a, hipStream_t st) {
+  const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 / WS);
+  hipLaunchKernelGGL((k_attn_dq<PL, DU, BN, WS, NST>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)),
+                     dim3(256), 0, st, a, int(tiles));
   return hipGetLastError();
+}
+template <int PL, int DU, int BM, int WS, int NST, bool VL>
+hipError_t dkv_of(const AttnArgs& a, hipStream_t st) {
+  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 / WS);
+  const int64_t grid = a.seqs.batch * a.kv_heads * a.kv_parts * tiles;
+  hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, WS, NST, VL>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a,
+                     int(tiles));
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.kv_parts == 1) return e;
+  const int64_t n = 2 * a.seqs.batch * int64_t(a.seqs.k_tokens) * a.kv_heads * (a.dim / 4);
+  hipLaunchKernelGGL((k_attn_sum_heads<typename Io<PL>::T>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+// How many waves share their rows (WS in the kernels): more than one where
+// workgroups of 128 rows would leave compute units idle and a row has enough to
+// pass over.  Measured on an MI355X, WS = 1 / 2 / 4, us:
+//   bf16, 48 workgroups, 512 keys of 64:       11.0 / 10.4 /  7.8 (gradients 31.9 / 24.9 / 20.4)
+//         128, 4096 keys of 128:               74.4 / 61.3 / 49.3 (276 / 205 / 152)
+//         128, a window of 256 in 2000:        13.5 / 11.2 / 20.1 (40 / 32 / 56)
+//         256, 4096 keys of 128:               78.1 / 66.5 / 95.9 (273 / 225 / 285)
+//         384, 700 keys of 96:                 17.8 / 20.8 / 46.5 (59 / 77 / 141)
+//   fp32 (4 where the head has up to 64 elements, else 2; one stage in LDS):
+//         32, 129 keys of 64 (gradients):      42.4 / - / 34.0
+//         256, 1024 keys of 128:               99.4 / 89.3 / - (338 / 249 / -)
+int waves_a_row(const AttnArgs& a, int dtype, int64_t workgroups, int64_t stream) {
+  if (a.causal && a.window) stream = std::min<int64_t>(stream, int64_t(a.window) + 128);
+  if (dtype != DT_BF16) return workgroups >= 512 || stream < 96 ? 1 : a.dim <= 64 ? 4 : 2;
+  if (workgroups >= 320 || stream < 256) return 1;
+  return workgroups < 256 && stream >= 512 ? 4 : 2;
+}
+
+// Kernels for heads of up to 64, 96 and 128 elements: those of up to 96 skip a
+// quarter of the products and LDS reads of 128.
+template <typename F>
+hipError_t by_width(int dim, F&& f) {
+  if (dim <= 64) return f(std::integral_constant<int, 64>{});
+  if (dim <= 96) return f(std::integral_constant<int, 96>{});
+  return f(std::integral_constant<int, 128>{});
 }
 
 }  // namespace
 
 int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window) {
-  if (s.q_off || (causal && window)) return 1;
+  if (s.q_off || (causal && window) || s.q_tokens > 128) return 1;
   const bool pack = packs_heads(s, q_heads / kv_heads);
   const int64_t items = s.batch * (pack ? int64_t(kv_heads) : q_heads * tiles_of(s, s.q_tokens, 128));
   if (items == 0 || items >= 256) return 1;
@@ -1305,13 +1423,16 @@ hipError_t run_attention_forward(AttnArgs a, int dtype, hipStream_t st, LaunchTi
   Timed tm(timer, KK_ATTENTION_FWD, st);
   hipError_t e = stage_sources(a, dtype, false, st);
   if (e != hipSuccess) return e;
-  const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
-  if (dtype == DT_BF16)
-    e = pick([&] { return forward_of<1, 64, 64>(a, st); }, [&] { return forward_of<1, 96, 64>(a, st); },
-             [&] { return forward_of<1, 128, 64>(a, st); });
-  else
-    e = pick([&] { return forward_of<3, 64, 32>(a, st); }, [&] { return forward_of<3, 96, 32>(a, st); },
-             [&] { return forward_of<3, 128, 32>(a, st); });
+  const bool pack = packs_heads(a.seqs, a.group);
+  const int64_t rows = pack ? int64_t(a.seqs.q_tokens) * a.group : a.seqs.q_tokens;
+  const int ws = waves_a_row(a, dtype, a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles_of(a.seqs, rows, 128) * a.splits,
+                             a.seqs.k_tokens / a.splits);
+  e = by_width(a.dim, [&](auto w) {
+    constexpr int DU = decltype(w)::value;
+    if (dtype != DT_BF16) return ws > 1 ? forward_of<3, DU, 32, DU <= 64 ? 4 : 2, 1>(a, st) : forward_of<3, DU, 32, 1, 2>(a, st);
+    if (ws == 4) return forward_of<1, DU, 32, 4, 2>(a, st);
+    return ws == 2 ? forward_of<1, DU, 32, 2, 2>(a, st) : forward_of<1, DU, 64, 1, 2>(a, st);
+  });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(4.0 * pairs_of(a) * a.dim, 0,
@@ -1324,14 +1445,23 @@ hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchT
   Timed tm(timer, KK_ATTENTION_BWD, st);
   hipError_t e = stage_sources(a, dtype, true, st);
   if (e != hipSuccess) return e;
-  const auto pick = [&](auto w64, auto w96, auto w128) { return a.dim <= 64 ? w64() : a.dim <= 96 ? w96() : w128(); };
-  if (dtype == DT_BF16)
-    e = pick([&] { return backward_of<1, 64, 64, 32, false>(a, st); },
-             [&] { return backward_of<1, 96, 64, 32, true>(a, st); }, [&] { return backward_of<1, 128, 64, 32, true>(a, st); });
-  else
-    e = pick([&] { return backward_of<3, 64, 32, 32, false>(a, st); },
-             [&] { return backward_of<3, 96, 32, 32, false>(a, st); },
-             [&] { return backward_of<3, 128, 32, 32, false>(a, st); });
+  const int ws_q = waves_a_row(a, dtype, a.seqs.batch * a.q_heads * tiles_of(a.seqs, a.seqs.q_tokens, 128), a.seqs.k_tokens);
+  const int ws_k = waves_a_row(a, dtype, a.seqs.batch * a.kv_heads * a.kv_parts * tiles_of(a.seqs, a.seqs.k_tokens, 128),
+                               int64_t(a.seqs.q_tokens) * (a.group / a.kv_parts));
+  e = by_width(a.dim, [&](auto w) {
+    constexpr int DU = decltype(w)::value, WS3 = DU <= 64 ? 4 : 2;
+    constexpr bool VL = DU > 64;
+    hipError_t r = hipSuccess;
+    if (a.seqs.q_tokens > 0) {
+      if (dtype != DT_BF16) r = ws_q > 1 ? dq_of<3, DU, 32, WS3, 1>(a, st) : dq_of<3, DU, 32, 1, 2>(a, st);
+      else if (ws_q == 4) r = dq_of<1, DU, 32, 4, 2>(a, st);
+      else r = ws_q == 2 ? dq_of<1, DU, 32, 2, 2>(a, st) : dq_of<1, DU, 64, 1, 2>(a, st);
+    }
+    if (r != hipSuccess || a.seqs.k_tokens == 0) return r;
+    if (dtype != DT_BF16) return ws_k > 1 ? dkv_of<3, DU, 32, WS3, 1, false>(a, st) : dkv_of<3, DU, 32, 1, 2, false>(a, st);
+    if (ws_k == 4) return dkv_of<1, DU, 32, 4, 2, VL>(a, st);
+    return ws_k == 2 ? dkv_of<1, DU, 32, 2, 2, VL>(a, st) : dkv_of<1, DU, 32, 1, 2, VL>(a, st);
+  });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)
     tm.done(10.0 * pairs_of(a) * a.dim, 0,
