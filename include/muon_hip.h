@@ -331,7 +331,8 @@ typedef struct {
  * behind a length get out = 0, lse = -inf and zero gradients, whatever their
  * inputs hold.  Packed: batch = 1, and q_offsets and k_offsets (device, int32,
  * [sequences + 1], not decreasing, both or neither) cut the token axes into
- * sequences; rows outside every sequence are left as they are.  Lengths and
+ * sequences; rows outside every sequence are left as they are (or see
+ * fill_rest).  Lengths and
  * offsets beyond the axes are cut to them.
  *
  * Inputs that are not finite propagate; one that only some queries of a
@@ -343,6 +344,9 @@ typedef struct {
   int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
   int32_t causal;          /* 0 or 1 */
   float scale;             /* finite, > 0 */
+  int32_t fill_rest;       /* packed: 1 writes zeros (lse: -inf) to the rows of
+                              outputs that no sequence holds; 0 leaves them */
+  int32_t reserved;        /* must be 0 */
   int64_t batch, q_tokens, k_tokens;
   int64_t sequences;       /* of a packed request, else 0 */
   int64_t window;          /* 0: none; otherwise needs causal */

@@ -83,7 +83,7 @@ class MuonHeads(ctypes.Structure):
 class MuonAttention(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("batch", ctypes.c_int64), ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
+                ("fill_rest", ctypes.c_int32), ("reserved", ctypes.c_int32), ("batch", ctypes.c_int64), ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
                 ("sequences", ctypes.c_int64), ("window", ctypes.c_int64),
                 ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
                 ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p),
@@ -377,7 +377,7 @@ def _stream_ptr(stream) -> int:
 # Requests of the attention block as packed records (a test compares them with
 # the ctypes layouts): filling ctypes fields takes longer than a small call.
 _HEADS = "Pqqq"
-_ATTENTION_PACK = struct.Struct("@iiiiif5q4P" + 5 * _HEADS + "PPPN")
+_ATTENTION_PACK = struct.Struct("@iiiiifii5q4P" + 5 * _HEADS + "PPPN")
 _GRAD_PACK = struct.Struct("@" + 4 * _HEADS)
 _ROTARY_PACK = struct.Struct("@iiiiifqqPqqqPii")
 _ROTARY_TENSOR_PACK = struct.Struct("@" + 2 * _HEADS + "q")
@@ -427,44 +427,51 @@ class _Attention:
         sk, hkv = k.shape[-3], k.shape[-2]
         self.lse_shape = (hq, sq) if packed else (batch, hq, sq)
         self.q_shape, self.k_shape = q.shape, k.shape
-        self.head = (self.code, d, hq, hkv, int(bool(causal)), float(d) ** -0.5 if scale is None else float(scale),
-                     batch, sq, sk, seqs, int(window),
+        self.start = (self.code, d, hq, hkv, int(bool(causal)), float(d) ** -0.5 if scale is None else float(scale))
+        self.head = (0, batch, sq, sk, seqs, int(window),
                      *(0 if t is None else t.data_ptr() for t in self.lists), *_heads(q), *_heads(k), *_heads(v))
 
-    def record(self, out, residual, lse, max_logits, scratch, scratch_bytes):
-        return _ATTENTION_PACK.pack(*self.head, *_heads(out), *(_NO_HEADS if residual is None else _heads(residual)),
+    def record(self, out, residual, lse, max_logits, scratch, scratch_bytes, fill=0):
+        return _ATTENTION_PACK.pack(*self.start, fill, *self.head, *_heads(out), *(_NO_HEADS if residual is None else _heads(residual)),
                                     lse.data_ptr(), 0 if max_logits is None else max_logits.data_ptr(), scratch,
                                     scratch_bytes)
 
     def sizes(self):
         """The record with no outputs yet, for muon_attention_scratch."""
-        return _ATTENTION_PACK.pack(*self.head, *_NO_HEADS, *_NO_HEADS, 0, 0, 0, 0)
+        return _ATTENTION_PACK.pack(*self.start, 0, *self.head, *_NO_HEADS, *_NO_HEADS, 0, 0, 0, 0)
 
 
 def _expect(t, shape, dtype, what):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
 
 
 def clip_records(wqs, wks, max_logits, threshold) -> bytes:
     """Packed entries of muon_qk_clip, their shapes checked (host only)."""
     import torch
-    recs = []
+    codes, f32 = {torch.float32: F32, torch.bfloat16: BF16}, torch.float32
+    threshold, pack, recs = float(threshold), _CLIP_PACK.pack, []
     for i, (q, k, m) in enumerate(zip(wqs, wks, max_logits)):
-        if q.dim() != 2 or k.dim() != 2 or q.shape[1] != k.shape[1] or q.dtype != k.dtype:
+        qs, ks, hq = q.shape, k.shape, m.numel()
+        if len(qs) != 2 or len(ks) != 2 or qs[1] != ks[1] or q.dtype is not k.dtype:
             raise ValueError(f"entry {i}: weights must be matrices of one dtype and one number of columns")
-        if m.dtype != torch.float32 or m.dim() != 1 or not m.is_contiguous() or m.numel() < 1:
+        if m.dtype is not f32 or m.dim() != 1 or hq < 1 or not m.is_contiguous():
             raise TypeError(f"entry {i}: logits must be a contiguous 1-D float32 tensor")
-        hq, (rows, cols) = m.numel(), q.shape
+        (rows, cols), rows_k = qs, ks[0]
         hd = rows // hq
-        if rows % hq or hd == 0 or k.shape[0] % hd or k.shape[0] == 0:
-            raise ValueError(f"entry {i}: {rows} query rows and {k.shape[0]} key rows are not whole heads of {hq}")
-        for t in (q, k):
-            if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
-                raise ValueError(f"entry {i}: rows must be contiguous and distinct")
-        recs.append(_CLIP_PACK.pack(q.data_ptr(), k.data_ptr(), m.data_ptr(), q.stride(0) if rows > 1 else cols,
-                                    k.stride(0) if k.shape[0] > 1 else cols, cols, hq, k.shape[0] // hd, hd,
-                                    _dtype_code(q), float(threshold), 0))
+        if rows % hq or hd == 0 or rows_k % hd or rows_k == 0:
+            raise ValueError(f"entry {i}: {rows} query rows and {rows_k} key rows are not whole heads of {hq}")
+        ldq = ldk = cols
+        if not (q.is_contiguous() and k.is_contiguous()):
+            for t in (q, k):
+                if (cols > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < cols):
+                    raise ValueError(f"entry {i}: rows must be contiguous and distinct")
+            ldq = q.stride(0) if rows > 1 else cols
+            ldk = k.stride(0) if rows_k > 1 else cols
+        code = codes.get(q.dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {q.dtype}")
+        recs.append(pack(q.data_ptr(), k.data_ptr(), m.data_ptr(), ldq, ldk, cols, hq, rows_k // hd, hd, code, threshold, 0))
     return b"".join(recs)
 
 
@@ -670,13 +677,13 @@ class Muon:
             if t is not None:
                 _expect(t, q.shape, q.dtype, what)
         keep, at, n = self._scratch(a.sizes(), 0, q)
-        if q_offsets is None:
-            out = q.new_empty(a.q_shape) if out is None else out
-            lse = q.new_empty(a.lse_shape, dtype=torch.float32)
-        else:  # rows outside packed sequences are not written
-            out = q.new_zeros(a.q_shape) if out is None else out
-            lse = q.new_full(a.lse_shape, -float("inf"), dtype=torch.float32)
-        self._check(self.lib.muon_attention_forward(self.h, a.record(out, residual, lse, max_logits, at, n),
+        # rows of no packed sequence: zeros in a new tensor, left alone in a given one
+        fill = int(q_offsets is not None and out is None)
+        out = q.new_empty(a.q_shape) if out is None else out
+        lse = q.new_empty(a.lse_shape, dtype=torch.float32)
+        if q_offsets is not None and not fill:
+            lse.fill_(-float("inf"))
+        self._check(self.lib.muon_attention_forward(self.h, a.record(out, residual, lse, max_logits, at, n, fill),
                                                     self._stream()))
         del keep
         return out, lse
@@ -704,12 +711,13 @@ class Muon:
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
         keep, at, n = self._scratch(a.sizes(), 1, q)
-        new = q.new_empty if q_offsets is None else q.new_zeros
+        fill = int(q_offsets is not None and dq is None and dk is None and dv is None)
+        new = q.new_zeros if q_offsets is not None and not fill else q.new_empty
         dq = new(a.q_shape) if dq is None else dq
         dk = new(a.k_shape) if dk is None else dk
         dv = new(a.k_shape) if dv is None else dv
         grad = _GRAD_PACK.pack(*_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv))
-        self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n), grad,
+        self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n, fill), grad,
                                                      self._stream()))
         del keep
         return dq, dk, dv

@@ -122,6 +122,9 @@ muon_status_t check_sizes(const muon_attention_t* a, Why& why) {
       a->k_tokens > kMaxTokens)
     return why.invalid("batch or tokens out of range");
   if (a->causal != 0 && a->causal != 1) return why.invalid("causal must be 0 or 1");
+  if ((a->fill_rest != 0 && a->fill_rest != 1) || (a->fill_rest && !a->q_offsets))
+    return why.invalid("fill_rest must be 0 or 1, and needs offsets");
+  if (a->reserved != 0) return why.invalid("reserved must be 0");
   if (!std::isfinite(a->scale) || !(a->scale > 0.f)) return why.invalid("scale must be finite and > 0");
   if (a->window < 0 || (a->window > 0 && !a->causal)) return why.invalid("window must be >= 0, and needs causal");
   if (!a->q_offsets != !a->k_offsets) return why.invalid("q_offsets and k_offsets go together");
@@ -263,6 +266,7 @@ muon_status_t check_attention(const muon_attention_t* a, const muon_attention_gr
   k.dim = a->head_dim;
   k.causal = a->causal;
   k.window = window_of(a);
+  k.fill = a->fill_rest;
   k.scale = a->scale;
   k.scale2 = float(double(a->scale) * 1.4426950408889634074);
   k.splits = p.splits;

@@ -32,6 +32,7 @@ struct AttnArgs {
   Seqs seqs;
   int32_t q_heads, kv_heads, group, dim;
   int32_t causal, window;
+  int32_t fill;              // packed: rows that no sequence holds get zeros (lse: -inf)
   float scale, scale2;       // scale2 = scale * log2(e)
   float* lse;                // [batch][q_heads][q_tokens], natural logarithm
   float* max_logits;         // [q_heads] or null

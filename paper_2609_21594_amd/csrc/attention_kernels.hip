@@ -117,14 +117,16 @@ struct Lay {
 template <int PL> struct Io { using T = uint16_t; };
 template <> struct Io<3> { using T = float; };
 template <int PL> struct Frag { u32x4_t v[PL]; };
-template <int PL>
+// SWAP: the operands are the other way round than in the pass that this one
+// has to agree with bit for bit; the products then come in its order.
+template <int PL, bool SWAP = false>
 __device__ __forceinline__ void mma(const Frag<PL>& a, const Frag<PL>& b, f32x16_t& c) {
   if constexpr (PL == 3) {
     Mma<uint16_t>::run(a.v[1], b.v[1], c);
-    Mma<uint16_t>::run(a.v[0], b.v[2], c);
-    Mma<uint16_t>::run(a.v[2], b.v[0], c);
-    Mma<uint16_t>::run(a.v[0], b.v[1], c);
-    Mma<uint16_t>::run(a.v[1], b.v[0], c);
+    Mma<uint16_t>::run(a.v[SWAP ? 2 : 0], b.v[SWAP ? 0 : 2], c);
+    Mma<uint16_t>::run(a.v[SWAP ? 0 : 2], b.v[SWAP ? 2 : 0], c);
+    Mma<uint16_t>::run(a.v[SWAP ? 1 : 0], b.v[SWAP ? 0 : 1], c);
+    Mma<uint16_t>::run(a.v[SWAP ? 0 : 1], b.v[SWAP ? 1 : 0], c);
   }
   Mma<uint16_t>::run(a.v[0], b.v[0], c);
 }
@@ -219,33 +221,6 @@ __device__ __forceinline__ void load_operand(const char* row, int dim, int half,
 #pragma unroll
   for (int s = 0; s < Lay<DU>::STEPS; ++s) f[s] = load_chunk<PL>(row, 2 * s + half, dim);
 }
-// The lane's half of the sum over the head of x * y, both as stored.
-template <int PL, int DU>
-__device__ __forceinline__ float dot_rows(const char* x, const char* y, int dim, int half) {
-  float r = 0.f;
-#pragma unroll
-  for (int s = 0; s < Lay<DU>::STEPS; ++s) {
-    const int c = 2 * s + half;
-    if constexpr (PL == 1) {
-      if (8 * c >= dim) continue;
-      const u32x4_t a = *reinterpret_cast<const u32x4_t*>(x + c * 16), b = *reinterpret_cast<const u32x4_t*>(y + c * 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        r = fmaf(__uint_as_float(a[k] << 16), __uint_as_float(b[k] << 16), r);
-        r = fmaf(__uint_as_float(a[k] & 0xffff0000u), __uint_as_float(b[k] & 0xffff0000u), r);
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        if (8 * c + 4 * q >= dim) continue;
-        const float4 a = *reinterpret_cast<const float4*>(x + c * 32 + q * 16), b = *reinterpret_cast<const float4*>(y + c * 32 + q * 16);
-        r = fmaf(a.x, b.x, r); r = fmaf(a.y, b.y, r); r = fmaf(a.z, b.z, r); r = fmaf(a.w, b.w, r);
-      }
-    }
-  }
-  return r;
-}
-
 // A operand of the contraction over the head: rows r0 + lane % 32 of a tile,
 // chunks 2 st + half.  As 2 st has no bit in common with half, the swizzled
 // address is a lane's base with bits flipped by a constant, plus a constant:
@@ -462,6 +437,26 @@ __device__ __forceinline__ Seq find_seq(const Seqs& s, int b, int tile, int bt, 
   return r;
 }
 
+// Packed: fills the rows of a head that no sequence holds, [0, first offset)
+// and [last offset, tokens), with zeros; the whole workgroup.
+__device__ __forceinline__ void outside_of(const Seqs& s, bool keys, int& lo, int& hi) {
+  const int32_t* off = keys ? s.k_off : s.q_off;
+  const int n = keys ? s.k_tokens : s.q_tokens;
+  lo = s.n_seq > 0 ? clampi(off[0], 0, n) : 0;
+  hi = s.n_seq > 0 ? clampi(off[s.n_seq], lo, n) : 0;
+}
+__device__ __forceinline__ void zero_outside(const Seqs& s, bool keys, const Heads& h, int head, int bytes) {
+  int lo, hi;
+  outside_of(s, keys, lo, hi);
+  const int n = keys ? s.k_tokens : s.q_tokens, chunks = bytes / 16;
+  const int64_t total = static_cast<int64_t>(lo + n - hi) * chunks;
+  for (int64_t i = threadIdx.x; i < total; i += 256) {
+    const int r = static_cast<int>(i / chunks), c = static_cast<int>(i % chunks);
+    const int64_t row = r < lo ? r : hi + r - lo;
+    *reinterpret_cast<u32x4_t*>(h.p + row * h.token + head * h.head + c * 16) = u32x4_t{0, 0, 0, 0};
+  }
+}
+
 __device__ __forceinline__ const char* at_row(const Heads& h, int b, int token, int head) {
   return h.p + b * h.batch + token * h.token + head * h.head;
 }
@@ -516,6 +511,16 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
     bid -= split * items;
   }
   const Item it = item_of(bid, a, pack ? 1 : a.group, tiles, a.causal);
+  if (a.fill && it.tile == tiles - 1) {  // one tile more than sequences can have
+    const int h = it.kvh * a.group + it.g;
+    zero_outside(a.seqs, false, a.out, h, a.dim * sizeof(T));
+    if (a.res.p) zero_outside(a.seqs, false, a.res, h, a.dim * sizeof(T));
+    int lo, hi;
+    outside_of(a.seqs, false, lo, hi);
+    for (int i = threadIdx.x; i < lo + a.seqs.q_tokens - hi; i += 256)
+      a.lse[row_index(a, 0, h, i < lo ? i : hi + i - lo)] = -kInf;
+    return;
+  }
   const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
@@ -804,6 +809,28 @@ __device__ __forceinline__ bool join_waves(f32x16_t* acc, char* smem, int wave, 
   return true;
 }
 
+// dout . (out + res) of the lane's row, as the diagonal of the products of 32
+// rows of out with those of dout: the same operation, in the same order, as
+// that of dout with a value row.  A row that sees one key has out equal to it
+// bit for bit, so its dP - delta, and with it its gradient, is exactly 0.
+template <int PL, int DU>
+__device__ __forceinline__ float row_dots(const Frag<PL>* df, const char* out, const char* res, int dim, int lane) {
+  const int half = lane >> 5, c = lane & 31;
+  f32x16_t p = zero16();
+#pragma unroll
+  for (int st = 0; st < Lay<DU>::STEPS; ++st) mma<PL>(load_chunk<PL>(out, 2 * st + half, dim), df[st], p);
+  if (res) {
+#pragma unroll
+    for (int st = 0; st < Lay<DU>::STEPS; ++st) mma<PL>(load_chunk<PL>(res, 2 * st + half, dim), df[st], p);
+  }
+  // column c's row c is in the half (c / 4) % 2, register 4 (c / 8) + c % 4
+  float x = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (e == 4 * (c >> 3) + (c & 3) && ((c >> 2) & 1) == half) x = p[e];
+  return sum32(x);
+}
+
 // dQ: a wave holds 32 queries (Q and dO rows in registers), the workgroup
 // passes over the keys: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 // First it forms each row's dout . out in fp32, with what the rounding took
@@ -822,6 +849,10 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ws = wave % WS, dch = (a.dim + 7) / 8;
   const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal);
+  if (a.fill && it.tile == tiles - 1) {
+    zero_outside(a.seqs, false, a.dq, it.kvh * a.group + it.g, a.dim * sizeof(T));
+    return;
+  }
   const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
@@ -851,9 +882,8 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
   const char* const dorow = at_row(a.dout, it.b, s.q0 + iq, head);
   load_operand<PL, DU>(at_row(a.q, it.b, s.q0 + iq, head), a.dim, half, qf);
   load_operand<PL, DU>(dorow, a.dim, half, df);
-  float delta = dot_rows<PL, DU>(dorow, at_row(a.out, it.b, s.q0 + iq, head), a.dim, half);
-  if (PL == 1 && a.res.p) delta += dot_rows<PL, DU>(dorow, at_row(a.res, it.b, s.q0 + iq, head), a.dim, half);
-  delta = sum32(delta);
+  const float delta = row_dots<PL, DU>(df, at_row(a.out, it.b, s.q0 + iq, head),
+                                       PL == 1 && a.res.p ? at_row(a.res, it.b, s.q0 + iq, head) : nullptr, a.dim, lane);
   const int64_t row = row_index(a, it.b, head, s.q0 + iq);
   const float lse = r < s.nq ? a.lse[row] : -kInf;
   const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
@@ -940,6 +970,13 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
   const int ws = wave % WS, dch = (a.dim + 7) / 8;
   const int heads = a.group / a.kv_parts;
   const Item it = item_of(blockIdx.x, a, a.kv_parts, tiles, false);
+  if (a.fill && it.tile == tiles - 1) {
+    if (a.kv_parts == 1) {  // (else the sum of the parts does)
+      zero_outside(a.seqs, true, a.dk, it.kvh, a.dim * sizeof(T));
+      zero_outside(a.seqs, true, a.dv, it.kvh, a.dim * sizeof(T));
+    }
+    return;
+  }
   const Seq s = find_seq(a.seqs, it.b, it.tile, BK, true);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
@@ -1022,12 +1059,12 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
       f32x16_t p = zero16(), d = zero16();
       wave_priority<PL == 1>();
 #pragma unroll
-      for (int st = 0; st < L::STEPS; ++st) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * qk * L::RB, st), kf[st], p);
+      for (int st = 0; st < L::STEPS; ++st) mma<PL, true>(frag_rows<PL, PLANE>(rb, 32 * qk * L::RB, st), kf[st], p);
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
         const Frag<PL> f = frag_rows<PL, PLANE>(rb, TILE + 32 * qk * L::RB, st);
-        if constexpr (VL) mma<PL>(f, frag_rows<PL, VPLANE>(vbase, 0, st), d);
-        else mma<PL>(f, vf[st], d);
+        if constexpr (VL) mma<PL, true>(f, frag_rows<PL, VPLANE>(vbase, 0, st), d);
+        else mma<PL, true>(f, vf[st], d);
       }
       interleave<PR * 2 * L::STEPS, PL * (VL ? 3 : 2) * L::STEPS, 6>();
       wave_priority<0>();
@@ -1101,12 +1138,16 @@ __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
   const int64_t kh = i / quads, tok = kh / a.kv_heads;
   const int head = static_cast<int>(kh % a.kv_heads);
   const int b = static_cast<int>(tok / a.seqs.k_tokens), j = static_cast<int>(tok % a.seqs.k_tokens);
-  if (a.seqs.q_off) {  // rows behind the last sequence stay as they are
-    if (j < a.seqs.k_off[0] || j >= a.seqs.k_off[a.seqs.n_seq]) return;
+  bool held = true;  // by a sequence
+  if (a.seqs.q_off) {
+    int lo, hi;
+    outside_of(a.seqs, true, lo, hi);
+    held = j >= lo && j < hi;
+    if (!held && !a.fill) return;
   }
   const float* p = (second ? a.part_dv : a.part_dk) + (tok * a.kv_heads + head) * a.kv_parts * a.dim + 4 * quad;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int g = 0; g < a.kv_parts; ++g, p += a.dim) {
+  for (int g = 0; g < a.kv_parts && held; ++g, p += a.dim) {
     const float4 y = *reinterpret_cast<const float4*>(p);
     x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
   }
@@ -1295,6 +1336,8 @@ __global__ __launch_bounds__(256) void k_reset_logits(ClipArgs a) {
 int64_t tiles_of(const Seqs& s, int64_t tokens, int bt) {
   return (tokens + bt - 1) / bt + (s.q_off ? s.n_seq : 0);
 }
+// The tiles of a launch: one more for the rows that no sequence holds.
+int64_t launch_tiles(const AttnArgs& a, int64_t tokens, int bt) { return tiles_of(a.seqs, tokens, bt) + (a.fill ? 1 : 0); }
 double pairs_of(const AttnArgs& a) {  // of a dense request, as an upper bound for packed ones
   const double nq = a.seqs.q_tokens, nk = a.seqs.k_tokens;
   return double(a.seqs.batch) * a.q_heads * nq * nk * (a.causal ? 0.5 : 1.0);
@@ -1338,7 +1381,7 @@ hipError_t stage_sources(AttnArgs& a, int dtype, bool backward, hipStream_t st) 
 template <int PL, int DU, int BN, int WS, int NST>
 hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   const bool pack = packs_heads(a.seqs, a.group);
-  const int64_t tiles = tiles_of(a.seqs, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 128 / WS);
+  const int64_t tiles = launch_tiles(a, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 128 / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
   const dim3 g(static_cast<unsigned>(grid)), b(256);
   if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, true>), g, b, 0, st, a, int(tiles), int(pack));
@@ -1352,14 +1395,14 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
 
 template <int PL, int DU, int BN, int WS, int NST>
 hipError_t dq_of(const AttnArgs& a, hipStream_t st) {
-  const int64_t tiles = tiles_of(a.seqs, a.seqs.q_tokens, 128 / WS);
+  const int64_t tiles = launch_tiles(a, a.seqs.q_tokens, 128 / WS);
   hipLaunchKernelGGL((k_attn_dq<PL, DU, BN, WS, NST>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)),
                      dim3(256), 0, st, a, int(tiles));
   return hipGetLastError();
 }
 template <int PL, int DU, int BM, int WS, int NST, bool VL>
 hipError_t dkv_of(const AttnArgs& a, hipStream_t st) {
-  const int64_t tiles = tiles_of(a.seqs, a.seqs.k_tokens, 128 / WS);
+  const int64_t tiles = launch_tiles(a, a.seqs.k_tokens, 128 / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * a.kv_parts * tiles;
   hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, WS, NST, VL>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a,
                      int(tiles));

@@ -163,6 +163,7 @@ BAD = [
     (dict(q_offsets=BASE, sequences=1), "together"), (dict(q_lengths=BASE), "together"),
     (dict(q_offsets=BASE, k_offsets=BASE, sequences=3), "batch 1"), (dict(sequences=2), "sequences"),
     (dict(q_offsets=BASE, k_offsets=BASE, q_lengths=BASE, k_lengths=BASE, batch=1), "exclude"),
+    (dict(fill_rest=1), "fill_rest"), (dict(fill_rest=2), "fill_rest"), (dict(reserved=1), "reserved"),
     (dict(q__data=0), "q is NULL"), (dict(k__data=BASE + 2), "k is not 16"), (dict(v__token_stride=130), "v: strides"),
     (dict(v__token_stride=-128), "v: stride"), (dict(q__token_stride=1 << 24), "token stride"),
     (dict(out__token_stride=64), "overlap"), (dict(out__batch_stride=0), "overlap"), (dict(out__data=BASE), "overlaps"),

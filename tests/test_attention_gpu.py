@@ -122,6 +122,16 @@ def test_backward(muon, case, dtype):
         assert np.array_equal(to_bits(x), to_bits(y))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_see_one_key_have_no_gradient(muon, dtype):
+    for b, s, h, hk, d, window in ((3, 1, 4, 2, 72, 0), (1, 300, 2, 1, 128, 1), (2, 40, 3, 3, 16, 1)):
+        q, k, v, do = make((b, s, s, h, hk, d, True, window), dtype)
+        want = ref.attention(*map(to_host, (q, k, v)), dtype, causal=True, window=window)
+        out, res, lse = saved(want, dtype)   # out is the value row, bit for bit
+        dq, dk, dv = muon.attention_backward(do, q, k, v, out, lse, residual=res, causal=True, window=window)
+        assert not dq.any() and not dk.any() and dv.any()
+
+
 def test_large_logits(muon):
     # logits of several hundred: one key takes nearly everything
     case = (1, 130, 130, 2, 2, 64, True, 0)
