@@ -130,14 +130,33 @@ __device__ __forceinline__ void mma(const Frag<PL>& a, const Frag<PL>& b, f32x16
   }
   Mma<uint16_t>::run(a.v[0], b.v[0], c);
 }
+// The same where b is an accumulator's operand: PA planes of it against one
+// bf16 operand (PL = 1), or as above.
+template <int PL, int PA>
+__device__ __forceinline__ void mma_acc(const Frag<PL>& a, const Frag<PA>& b, f32x16_t& c) {
+  if constexpr (PL == 3) {
+    mma<3>(a, b, c);
+  } else {
+#pragma unroll
+    for (int p = PA - 1; p >= 0; --p) Mma<uint16_t>::run(a.v[0], b.v[p], c);
+  }
+}
+// Planes that probabilities and their gradients are taken in as operands: one
+// rounding to bf16 (2^-9 of each, as much as the result's own rounding costs),
+// three for fp32.  FINE: two, so that what is left is 2^-17; for requests of
+// few rows (fine_of), where single roundings do not average out and the
+// products cost little.
+template <int PL, bool FINE> constexpr int kAccPlanes = PL == 3 ? 3 : FINE ? 2 : 1;
 // A pair of values as words of the planes.
 template <int PL>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t* w) {
   w[0] = pack_bf16x2(x, y);
-  if constexpr (PL == 3) {
+  if constexpr (PL >= 2) {
     x -= __uint_as_float(w[0] << 16);
     y -= __uint_as_float(w[0] & 0xffff0000u);
     w[1] = pack_bf16x2(x, y);
+  }
+  if constexpr (PL == 3) {
     x -= __uint_as_float(w[1] << 16);
     y -= __uint_as_float(w[1] & 0xffff0000u);
     w[2] = pack_bf16x2(x, y);
@@ -493,9 +512,10 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 // share their queries and take every WS-th tile, and are joined at the end; for
 // requests with too few rows to fill the device.
 // ---------------------------------------------------------------------------
-template <int PL, int DU, int BN, int WS, int NST, bool SPLIT>
+template <int PL, int DU, int BN, int WS, int NST, bool FINE, bool SPLIT>
 __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
-  constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
+  constexpr int PA = kAccPlanes<PL, FINE>;
+  constexpr int PR = PL == 3 ? 6 : 1, PP = PL == 3 ? 6 : PA;  // MFMAs of a product, and of one with an accumulator
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
   constexpr int BM = 128 / WS, KB = BN / 32, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
@@ -639,12 +659,12 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const Frag<PL> pf = frag_acc<PL>(p[kb], st);
+        const Frag<PA> pf = frag_acc<PA>(p[kb], st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db)
-          mma<PL>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * kb * L::RB, st, db), pf, o[db]);
+          mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * kb * L::RB, st, db), pf, o[db]);
       }
-    interleave<PR * KB * 2 * L::DB, PL * KB * 4 * L::DB, 8>();
+    interleave<PP * KB * 2 * L::DB, PL * KB * 4 * L::DB, 8>();
     __builtin_amdgcn_sched_barrier(0);
   }
 
@@ -837,9 +857,10 @@ __device__ __forceinline__ float row_dots(const Frag<PL>* df, const char* out, c
 // from out where the caller kept it, and writes it and log2 of the sum of
 // exponentials for k_attn_dkv: +inf where no key is visible, so that every
 // probability recomputed from it is 0.
-template <int PL, int DU, int BN, int WS, int NST>
+template <int PL, int DU, int BN, int WS, int NST, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
-  constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
+  constexpr int PA = kAccPlanes<PL, FINE>;
+  constexpr int PR = PL == 3 ? 6 : 1, PP = PL == 3 ? 6 : PA;  // MFMAs of a product, and of one with an accumulator
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
   constexpr int BM = 128 / WS, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
@@ -931,12 +952,12 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
       wave_priority<PL == 1>();
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const Frag<PL> f = frag_acc<PL>(d, st);
+        const Frag<PA> f = frag_acc<PA>(d, st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db)
-          mma<PL>(frag_cols<PL, DU, PLANE>(cb, 32 * kb * L::RB, st, db), f, acc[db]);
+          mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, 32 * kb * L::RB, st, db), f, acc[db]);
       }
-      interleave<PR * 2 * L::DB, PL * 4 * L::DB, 6>();
+      interleave<PP * 2 * L::DB, PL * 4 * L::DB, 6>();
       wave_priority<0>();
     }
   }
@@ -953,9 +974,10 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
 // dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in
 // LDS), the workgroup passes over the queries of one head, or of several heads
 // of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
-template <int PL, int DU, int BM, int WS, int NST, bool VL>
+template <int PL, int DU, int BM, int WS, int NST, bool VL, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
-  constexpr int PR = PL == 3 ? 6 : 1;  // MFMAs of a product
+  constexpr int PA = kAccPlanes<PL, FINE>;
+  constexpr int PR = PL == 3 ? 6 : 1, PP = PL == 3 ? 6 : PA;  // MFMAs of a product, and of one with an accumulator
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
   constexpr int BK = 128 / WS, SR = BM * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
@@ -1091,18 +1113,18 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
       wave_priority<PL == 1>();
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const Frag<PL> f = frag_acc<PL>(p, st);
+        const Frag<PA> f = frag_acc<PA>(p, st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db)
-          mma<PL>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * qk * L::RB, st, db), f, dv[db]);
+          mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * qk * L::RB, st, db), f, dv[db]);
       }
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const Frag<PL> f = frag_acc<PL>(d, st);
+        const Frag<PA> f = frag_acc<PA>(d, st);
 #pragma unroll
-        for (int db = 0; db < L::DB; ++db) mma<PL>(frag_cols<PL, DU, PLANE>(cb, 32 * qk * L::RB, st, db), f, dk[db]);
+        for (int db = 0; db < L::DB; ++db) mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, 32 * qk * L::RB, st, db), f, dk[db]);
       }
-      interleave<PR * 4 * L::DB, PL * 8 * L::DB, 6>();
+      interleave<PP * 4 * L::DB, PL * 8 * L::DB, 6>();
       wave_priority<0>();
     }
   }
@@ -1378,14 +1400,14 @@ hipError_t stage_sources(AttnArgs& a, int dtype, bool backward, hipStream_t st) 
   return hipGetLastError();
 }
 
-template <int PL, int DU, int BN, int WS, int NST>
+template <int PL, int DU, int BN, int WS, int NST, bool FINE = false>
 hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   const bool pack = packs_heads(a.seqs, a.group);
   const int64_t tiles = launch_tiles(a, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 128 / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
   const dim3 g(static_cast<unsigned>(grid)), b(256);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, true>), g, b, 0, st, a, int(tiles), int(pack));
-  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, false>), g, b, 0, st, a, int(tiles), int(pack));
+  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, true>), g, b, 0, st, a, int(tiles), int(pack));
+  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, false>), g, b, 0, st, a, int(tiles), int(pack));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
@@ -1393,18 +1415,18 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int PL, int DU, int BN, int WS, int NST>
+template <int PL, int DU, int BN, int WS, int NST, bool FINE = false>
 hipError_t dq_of(const AttnArgs& a, hipStream_t st) {
   const int64_t tiles = launch_tiles(a, a.seqs.q_tokens, 128 / WS);
-  hipLaunchKernelGGL((k_attn_dq<PL, DU, BN, WS, NST>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)),
+  hipLaunchKernelGGL((k_attn_dq<PL, DU, BN, WS, NST, FINE>), dim3(static_cast<unsigned>(a.seqs.batch * a.q_heads * tiles)),
                      dim3(256), 0, st, a, int(tiles));
   return hipGetLastError();
 }
-template <int PL, int DU, int BM, int WS, int NST, bool VL>
+template <int PL, int DU, int BM, int WS, int NST, bool VL, bool FINE = false>
 hipError_t dkv_of(const AttnArgs& a, hipStream_t st) {
   const int64_t tiles = launch_tiles(a, a.seqs.k_tokens, 128 / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * a.kv_parts * tiles;
-  hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, WS, NST, VL>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a,
+  hipLaunchKernelGGL((k_attn_dkv<PL, DU, BM, WS, NST, VL, FINE>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a,
                      int(tiles));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.kv_parts == 1) return e;
@@ -1431,6 +1453,14 @@ int waves_a_row(const AttnArgs& a, int dtype, int64_t workgroups, int64_t stream
   if (workgroups >= 320 || stream < 256) return 1;
   return workgroups < 256 && stream >= 512 ? 4 : 2;
 }
+
+// Whether probabilities and their gradients are taken in two planes: where the
+// rows are few.  With one, an output's error is 1.4 times that of the exact one
+// rounded (2^-9 of each probability beside 2^-9 of the result), on average; of
+// 300 random requests 7 with up to 4096 rows came to 1.5 to 2.  Query gradients
+// of heads of up to 32 elements too: the few keys that a query selects resemble
+// each other there, their terms cancel, and one plane leaves 1.6 times.
+bool fine_of(const AttnArgs& a) { return a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens) <= 4096; }
 
 // Kernels for heads of up to 64, 96 and 128 elements: those of up to 96 skip a
 // quarter of the products and LDS reads of 128.
@@ -1473,6 +1503,7 @@ hipError_t run_attention_forward(AttnArgs a, int dtype, hipStream_t st, LaunchTi
   e = by_width(a.dim, [&](auto w) {
     constexpr int DU = decltype(w)::value;
     if (dtype != DT_BF16) return ws > 1 ? forward_of<3, DU, 32, DU <= 64 ? 4 : 2, 1>(a, st) : forward_of<3, DU, 32, 1, 2>(a, st);
+    if (fine_of(a)) return ws == 4 ? forward_of<1, DU, 32, 4, 2, true>(a, st) : forward_of<1, DU, 64, 1, 2, true>(a, st);
     if (ws == 4) return forward_of<1, DU, 32, 4, 2>(a, st);
     return ws == 2 ? forward_of<1, DU, 32, 2, 2>(a, st) : forward_of<1, DU, 64, 1, 2>(a, st);
   });
@@ -1497,11 +1528,13 @@ hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchT
     hipError_t r = hipSuccess;
     if (a.seqs.q_tokens > 0) {
       if (dtype != DT_BF16) r = ws_q > 1 ? dq_of<3, DU, 32, WS3, 1>(a, st) : dq_of<3, DU, 32, 1, 2>(a, st);
+      else if (fine_of(a) || a.dim <= 32) r = ws_q == 4 ? dq_of<1, DU, 32, 4, 2, true>(a, st) : dq_of<1, DU, 64, 1, 2, true>(a, st);
       else if (ws_q == 4) r = dq_of<1, DU, 32, 4, 2>(a, st);
       else r = ws_q == 2 ? dq_of<1, DU, 32, 2, 2>(a, st) : dq_of<1, DU, 64, 1, 2>(a, st);
     }
     if (r != hipSuccess || a.seqs.k_tokens == 0) return r;
     if (dtype != DT_BF16) return ws_k > 1 ? dkv_of<3, DU, 32, WS3, 1, false>(a, st) : dkv_of<3, DU, 32, 1, 2, false>(a, st);
+    if (fine_of(a)) return ws_k == 4 ? dkv_of<1, DU, 32, 4, 2, VL, true>(a, st) : dkv_of<1, DU, 32, 1, 2, VL, true>(a, st);
     if (ws_k == 4) return dkv_of<1, DU, 32, 4, 2, VL>(a, st);
     return ws_k == 2 ? dkv_of<1, DU, 32, 2, 2, VL>(a, st) : dkv_of<1, DU, 32, 1, 2, VL>(a, st);
   });
