@@ -56,6 +56,9 @@ __device__ __forceinline__ float wave_max(float x) {
 // NaN.  Maxima do not depend on the order of the updates.
 __device__ __forceinline__ void atomic_max_f32(float* p, float x) {
   x += 0.f;  // no negative zero
+  // (most updates change nothing, and thousands of atomics on one cache line
+  // take longer than a pass over short sequences: look first)
+  if (!(x > __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))) return;
   if (x >= 0.f) atomicMax(reinterpret_cast<int*>(p), __float_as_int(x));
   else atomicMin(reinterpret_cast<unsigned*>(p), __float_as_uint(x));
 }
