@@ -67,6 +67,8 @@ class MuonAdamW(torch.optim.Optimizer):
         for t in (wq, wk, max_logits):
             if t.device.type != "cuda" or (t.device.index or 0) != self._device:
                 raise ValueError("clip_query_keys needs tensors on the parameters' GPU")
+        # (a view of a parameter would keep an autograd graph of it alive)
+        wq, wk = (w if w.is_leaf else w.detach() for w in (wq, wk))
         entry = (wq, wk, max_logits, float(threshold))
         params = {p.untyped_storage().data_ptr() for g in self.param_groups for p in g["params"]}
         if any(w.untyped_storage().data_ptr() not in params for w in entry[:2]):
