@@ -409,10 +409,30 @@ struct Seq { int q0, nq, k0, nk, q_rows, k_rows, tile; bool ok; };
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
-// The sequence that holds tile `tile` of `bt` queries (keys where by_key).
-// Packed: the tiles of all sequences are numbered one after the other; each
-// wave counts them, 64 sequences at a time.
-__device__ __forceinline__ Seq find_seq(const Seqs& s, int b, int tile, int bt, bool by_key) {
+// Sum over the wave's lanes of non-negative numbers below 2^bits, by bit planes.
+__device__ __forceinline__ int wave_count(int x, int bits) {
+  int sum = 0;
+  for (int b = 0; b < bits; ++b) sum += __popcll(__ballot((x >> b) & 1)) << b;
+  return sum;
+}
+
+// The sequence that holds tile `tile` (of `tiles`) of `bt` queries, or keys
+// where by_key.  Packed, each wave finds it from the offsets, the tiles being
+// numbered in one of two ways:
+//   - sequence s has the numbers from offset / bt + s on: its tiles and at most
+//     one number without work, so that a search finds it, 64 probes at a time
+//     (4000 sequences of 32 tokens x 8 heads of 64: 225 us forward; 924 where
+//     each wave added up the tiles of all sequences before its own).  Numbers are
+//     taken in another order inside each 64: those without work often alternate
+//     with the others, and a launch deals its workgroups out to the parts of an
+//     XCD in turn (256 sequences of 128: 32 us, 43 in the numbers' order);
+//   - ranked (causal, up to 64 sequences: a lane for each): by the number of
+//     keys that a tile passes over, largest first.  By sequence, the launch would
+//     end with the long tiles of one sequence (8 sequences of 4096 x 8 heads of
+//     64: 194 us forward, 221 so).
+__device__ __forceinline__ bool ranks_tiles(const AttnArgs& a) { return a.seqs.q_off && a.causal && a.seqs.n_seq <= 64; }
+__device__ __forceinline__ Seq find_seq(const AttnArgs& a, int b, int tile, int tiles, int bt, bool by_key) {
+  const Seqs& s = a.seqs;
   Seq r;
   r.ok = true;
   r.tile = tile;
@@ -425,37 +445,57 @@ __device__ __forceinline__ Seq find_seq(const Seqs& s, int b, int tile, int bt, 
     return r;
   }
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int s0 = 0; s0 < s.n_seq; s0 += 64) {
-    const int i = s0 + lane;
-    int q0 = 0, nq = 0, k0 = 0, nk = 0;
-    if (i < s.n_seq) {
-      q0 = clampi(s.q_off[i], 0, s.q_tokens);
-      nq = clampi(s.q_off[i + 1], q0, s.q_tokens) - q0;
-      k0 = clampi(s.k_off[i], 0, s.k_tokens);
-      nk = clampi(s.k_off[i + 1], k0, s.k_tokens) - k0;
-    }
-    const int n = ((by_key ? nk : nq) + bt - 1) / bt;
-    int upto = n;  // tiles of this lane's sequence and those before it
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
-    }
-    const unsigned long long hit = __ballot(before + upto > tile);
-    if (hit) {
-      const int l = __ffsll(hit) - 1;
-      r.tile = tile - before - __builtin_amdgcn_readlane(upto - n, l);
-      r.q0 = __builtin_amdgcn_readlane(q0, l);
-      r.nq = r.q_rows = __builtin_amdgcn_readlane(nq, l);
-      r.k0 = __builtin_amdgcn_readlane(k0, l);
-      r.nk = r.k_rows = __builtin_amdgcn_readlane(nk, l);
-      return r;
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
+  const bool ranked = ranks_tiles(a);
+  if (!ranked && tile < (tiles & ~63)) tile = (tile & ~63) | (tile & 7) << 3 | (tile >> 3 & 7);
+  // the search, down to 64 sequences from `lo` on, one a lane
+  int lo = 0, n = s.n_seq;
+  while (n > 64) {
+    const int32_t* off = by_key ? s.k_off : s.q_off;
+    const int step = (n + 63) >> 6, i = lo + lane * step;
+    const bool start = lane * step < n && clampi(off[i], 0, by_key ? s.k_tokens : s.q_tokens) / bt + i <= tile;
+    const int skip = max(__popcll(__ballot(start)) - 1, 0) * step;
+    lo += skip;
+    n = min(n - skip, step);
   }
-  r.q0 = r.nq = r.k0 = r.nk = r.q_rows = r.k_rows = 0;
-  r.ok = false;
+  int q0 = 0, nq = 0, k0 = 0, nk = 0;
+  if (lane < n) {
+    const int32_t *qo = s.q_off + lo + lane, *ko = s.k_off + lo + lane;
+    const int qa = qo[0], qb = qo[1], ka = ko[0], kb = ko[1];
+    q0 = clampi(qa, 0, s.q_tokens);
+    nq = clampi(qb, q0, s.q_tokens) - q0;
+    k0 = clampi(ka, 0, s.k_tokens);
+    nk = clampi(kb, k0, s.k_tokens) - k0;
+  }
+  unsigned long long hit;
+  if (ranked) {
+    const int mine = ((by_key ? nk : nq) + bt - 1) / bt;
+    // level i: the i-th tiles of all sequences that have it; above(i): the tiles
+    // of higher levels.  The number's level is the lowest with above(i) <= tile.
+    const int top = (by_key ? s.k_tokens : s.q_tokens) / bt + 1, bits = 32 - __clz(top);
+    int level = 0, end = top;
+    while (level < end) {
+      const int mid = (level + end) >> 1;
+      if (wave_count(max(mine - mid - 1, 0), bits) <= tile) end = mid;
+      else level = mid + 1;
+    }
+    const unsigned long long have = __ballot(mine > level);
+    const int nth = tile - wave_count(max(mine - level - 1, 0), bits);
+    const int below = __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(have >> 32),
+                                                __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(have), 0));
+    hit = __ballot(mine > level && below == nth);
+    r.tile = by_key ? mine - 1 - level : level;
+  } else {
+    r.tile = tile - (by_key ? k0 : q0) / bt - lo - lane;
+    const int starts = __popcll(__ballot(lane < n && r.tile >= 0));
+    hit = starts ? 1ull << (starts - 1) : 0;
+  }
+  const int at = hit ? __ffsll(hit) - 1 : 0;
+  r.tile = __builtin_amdgcn_readlane(r.tile, at);
+  r.q0 = __builtin_amdgcn_readlane(q0, at);
+  r.nq = r.q_rows = __builtin_amdgcn_readlane(nq, at);
+  r.k0 = __builtin_amdgcn_readlane(k0, at);
+  r.nk = r.k_rows = __builtin_amdgcn_readlane(nk, at);
+  r.ok = hit && r.tile * bt < (by_key ? r.nk : r.nq);
   return r;
 }
 
@@ -533,7 +573,7 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
     split = bid / items;
     bid -= split * items;
   }
-  const Item it = item_of(bid, a, pack ? 1 : a.group, tiles, a.causal);
+  const Item it = item_of(bid, a, pack ? 1 : a.group, tiles, a.causal && !ranks_tiles(a));
   if (a.fill && it.tile == tiles - 1) {  // one tile more than sequences can have
     const int h = it.kvh * a.group + it.g;
     zero_outside(a.seqs, false, a.out, h, a.dim * sizeof(T));
@@ -544,7 +584,7 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
       a.lse[row_index(a, 0, h, i < lo ? i : hi + i - lo)] = -kInf;
     return;
   }
-  const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
+  const Seq s = find_seq(a, it.b, it.tile, tiles, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
 
@@ -872,12 +912,12 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ws = wave % WS, dch = (a.dim + 7) / 8;
-  const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal);
+  const Item it = item_of(blockIdx.x, a, a.group, tiles, a.causal && !ranks_tiles(a));
   if (a.fill && it.tile == tiles - 1) {
     zero_outside(a.seqs, false, a.dq, it.kvh * a.group + it.g, a.dim * sizeof(T));
     return;
   }
-  const Seq s = find_seq(a.seqs, it.b, it.tile, BM, false);
+  const Seq s = find_seq(a, it.b, it.tile, tiles, BM, false);
   if (!s.ok) return;
   const int shift = s.nk - s.nq, head = it.kvh * a.group + it.g;
   const int r0 = s.tile * BM + wave / WS * 32;
@@ -1002,7 +1042,7 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
     }
     return;
   }
-  const Seq s = find_seq(a.seqs, it.b, it.tile, BK, true);
+  const Seq s = find_seq(a, it.b, it.tile, tiles, BK, true);
   if (!s.ok) return;
   const int shift = s.nk - s.nq;
   const int k0 = s.tile * BK, w0 = k0 + wave / WS * 32;

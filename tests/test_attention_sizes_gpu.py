@@ -1,0 +1,112 @@
+"""Attention requests of the sizes from which a launch takes another form: many
+rows (probabilities in one bf16 plane), many and few workgroups (a wave to a row
+or several), heads of a group in parts or added up at once, many sequences."""
+import numpy as np
+import pytest
+
+from oracle import attention_ref as ref
+from tests.gpu_util import to_bits, to_host
+from tests.test_attention_gpu import close, make, muon, saved  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+
+# dtype and batch, queries, keys, query heads, key heads, head size, causal, window
+SIZES = [
+    # bf16, more than 4096 rows
+    ("bf16", 20, 130, 130, 16, 4, 64, True, 0),     # 640 workgroups of queries
+    ("bf16", 20, 130, 130, 16, 4, 32, False, 0),
+    ("bf16", 22, 129, 70, 16, 16, 96, True, 0),
+    ("bf16", 10, 131, 140, 16, 2, 128, True, 50),
+    ("bf16", 4, 300, 301, 4, 2, 64, True, 0),       # 48, over 301 keys
+    ("bf16", 4, 300, 301, 4, 4, 128, False, 0),
+    ("bf16", 9, 400, 260, 8, 8, 24, True, 0),       # 288
+    ("bf16", 2, 600, 700, 4, 2, 64, True, 0),       # 40, over 700
+    ("bf16", 2, 600, 700, 4, 1, 96, True, 0),
+    ("bf16", 2, 533, 520, 4, 2, 128, False, 0),
+    ("bf16", 1, 1100, 1100, 4, 2, 80, True, 200),
+    ("bf16", 2, 4097, 1, 1, 1, 16, False, 0),       # one key
+    # the heads of a group: each by itself, two parts, all at once
+    ("bf16", 32, 33, 130, 32, 8, 16, True, 0),
+    ("bf16", 64, 40, 130, 16, 8, 16, True, 0),
+    ("f32", 32, 33, 130, 32, 8, 16, True, 0),
+    ("f32", 64, 40, 130, 16, 8, 16, False, 0),
+    # fp32: 512 workgroups and more
+    ("f32", 32, 65, 100, 16, 4, 64, True, 0),
+    ("f32", 32, 40, 99, 16, 16, 72, False, 0),
+    ("f32", 32, 40, 99, 16, 4, 128, True, 30),
+    ("f32", 1, 600, 500, 2, 1, 96, True, 0),
+]
+
+
+@pytest.mark.parametrize("case", SIZES, ids=str)
+def test_sizes(muon, case):
+    dtype, case = case[0], case[1:]
+    q, k, v, do = make(case, dtype, 1.5)
+    kw = dict(causal=case[6], window=case[7])
+    want = ref.attention(*map(to_host, (q, k, v)), dtype, dout=to_host(do), **kw)
+    got, lse = muon.attention(q, k, v, **kw)
+    close(got, want["out"], "out")
+    close(lse, want["lse"], "lse")
+    out, res, lse = saved(want, dtype)
+    got = muon.attention_backward(do, q, k, v, out, lse, residual=res, **kw)
+    for name, x in zip(("dq", "dk", "dv"), got):
+        close(x, want[name], name)
+    again = muon.attention_backward(do, q, k, v, out, lse, residual=res, **kw)
+    for x, y in zip(got, again):
+        assert np.array_equal(to_bits(x), to_bits(y))
+
+
+# lengths of the sequences (keys: the same, or those after the colon), heads of queries and keys, head size
+PACKED = [
+    ([1, 500, 0, 3, 129, 128, 127], None, 4, 2, 64),
+    ([300] + [0] * 62 + [5], None, 4, 4, 32),                         # 64
+    ([2, 0, 1] * 21 + [140, 7], None, 4, 1, 72),                      # 65
+    ([3, 0, 9, 131, 1] * 40, [2, 4, 0, 140, 7] * 40, 4, 2, 32),       # 200
+    ([4] * 130, None, 16, 8, 64),                                     # the heads of a group added up at once
+    ([1] * 4000 + [0] * 90 + [3] * 30, None, 2, 1, 16),               # two rounds of a search
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 100)])
+@pytest.mark.parametrize("index", range(len(PACKED)))
+def test_packed(muon, index, causal, window, dtype):
+    import torch
+    nq, nk, hq, hkv, d = PACKED[index]
+    nk = nk or nq
+    qo, ko = np.cumsum([3] + nq), np.cumsum([0] + nk)
+    sq, sk = int(qo[-1]) + 2, int(ko[-1]) + 5
+    q, k, v, do = make((1, sq, sk, hq, hkv, d, causal, window), dtype)
+    seqs = [(0, int(a), n, int(b), m) for a, n, b, m in zip(qo, nq, ko, nk)]
+    want = ref.attention(*map(to_host, (q, k, v)), dtype, causal=causal, window=window, seqs=seqs, dout=to_host(do))
+    out, res, lse = saved(want, dtype)
+    kw = dict(causal=causal, window=window, q_offsets=torch.from_numpy(qo.astype(np.int32)).cuda(),
+              k_offsets=torch.from_numpy(ko.astype(np.int32)).cuda())
+    q, k, v, do = (t[0] for t in (q, k, v, do))
+    o, l = muon.attention(q, k, v, **kw)
+    close(o, want["out"], "out")
+    close(l, want["lse"], "lse")
+    got = muon.attention_backward(do, q, k, v, out[0], lse[0], residual=None if res is None else res[0], **kw)
+    for name, x in zip(("dq", "dk", "dv"), got):
+        close(x, want[name], name)
+
+
+def test_offsets_out_of_order_stay_inside_the_tensors(muon):
+    """Not a sequence list, so no result is right; nothing beyond the tensors is written."""
+    import torch
+    rng = np.random.default_rng(3)
+    t = 700
+    for n in (5, 64, 65, 300):
+        q, k, v, do = (torch.full((t + 200, 2, 32), 3.0, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+        bad = [torch.from_numpy(rng.integers(-900, 1500, n + 1).astype(np.int32)).cuda() for _ in range(2)]
+        kw = dict(causal=True, q_offsets=bad[0], k_offsets=bad[1])
+        given = [torch.full_like(q, 5.0) for _ in range(4)]
+        part = slice(100, 100 + t)
+        _, lse = muon.attention(q[part], k[part], v[part], out=given[0][part], **kw)
+        lse.zero_()
+        muon.attention_backward(do[part], q[part], k[part], v[part], q[part], lse, dq=given[1][part], dk=given[2][part],
+                                dv=given[3][part], **kw)
+        for x in given:
+            assert (x[:100] == 5).all() and (x[100 + t:] == 5).all()
