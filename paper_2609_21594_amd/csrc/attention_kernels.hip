@@ -418,19 +418,23 @@ __device__ __forceinline__ int wave_count(int x, int bits) {
 
 // The sequence that holds tile `tile` (of `tiles`) of `bt` queries, or keys
 // where by_key.  Packed, each wave finds it from the offsets, the tiles being
-// numbered in one of two ways:
-//   - sequence s has the numbers from offset / bt + s on: its tiles and at most
-//     one number without work, so that a search finds it, 64 probes at a time
-//     (4000 sequences of 32 tokens x 8 heads of 64: 225 us forward; 924 where
-//     each wave added up the tiles of all sequences before its own).  Numbers are
-//     taken in another order inside each 64: those without work often alternate
-//     with the others, and a launch deals its workgroups out to the parts of an
-//     XCD in turn (256 sequences of 128: 32 us, 43 in the numbers' order);
-//   - ranked (causal, up to 64 sequences: a lane for each): by the number of
-//     keys that a tile passes over, largest first.  By sequence, the launch would
-//     end with the long tiles of one sequence (8 sequences of 4096 x 8 heads of
-//     64: 194 us forward, 221 so).
-__device__ __forceinline__ bool ranks_tiles(const AttnArgs& a) { return a.seqs.q_off && a.causal && a.seqs.n_seq <= 64; }
+// numbered in one of three ways:
+//   - more than 64 sequences: sequence s has the numbers from offset / bt + s on,
+//     its tiles and at most one number without work, so that a search finds it,
+//     64 probes at a time (4000 sequences of 32 tokens x 8 heads of 64: 225 us
+//     forward; 924 where each wave added up the tiles of all sequences before
+//     its own).  Numbers are taken in another order inside each 64: those without
+//     work often alternate with the others, and a launch deals its workgroups out
+//     to the parts of an XCD in turn (256 sequences of 128: 32 us, 43 in the
+//     numbers' order);
+//   - up to 64, a lane for each, causal without a window: by the number of keys
+//     that a tile passes over, largest first.  By sequence, the launch would end
+//     with the long tiles of one (8 sequences of 4096 x 8 heads of 64: 194 us
+//     forward, 221 by sequence);
+//   - otherwise one sequence's after the other's, which keeps the tiles that read
+//     the same keys together (11 sequences of 745 x 16 heads of 64, a window of 1024:
+//     45 us forward, 52 ranked, 51 in the order of many).
+__device__ __forceinline__ bool ranks_tiles(const AttnArgs& a) { return a.seqs.q_off && a.causal && !a.window && a.seqs.n_seq <= 64; }
 __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int b, int tile, int tiles, int bt, bool by_key) {
   const Seqs& s = a.seqs;
   Seq r;
@@ -445,8 +449,8 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int b, int tile, int 
     return r;
   }
   const int lane = threadIdx.x & 63;
-  const bool ranked = ranks_tiles(a);
-  if (!ranked && tile < (tiles & ~63)) tile = (tile & ~63) | (tile & 7) << 3 | (tile >> 3 & 7);
+  const bool many = s.n_seq > 64;
+  if (many && tile < (tiles & ~63)) tile = (tile & ~63) | (tile & 7) << 3 | (tile >> 3 & 7);
   // the search, down to 64 sequences from `lo` on, one a lane
   int lo = 0, n = s.n_seq;
   while (n > 64) {
@@ -467,8 +471,12 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int b, int tile, int 
     nk = clampi(kb, k0, s.k_tokens) - k0;
   }
   unsigned long long hit;
-  if (ranked) {
-    const int mine = ((by_key ? nk : nq) + bt - 1) / bt;
+  const int mine = ((by_key ? nk : nq) + bt - 1) / bt;
+  if (many) {
+    r.tile = tile - (by_key ? k0 : q0) / bt - lo - lane;
+    const int starts = __popcll(__ballot(lane < n && r.tile >= 0));
+    hit = starts ? 1ull << (starts - 1) : 0;
+  } else if (ranks_tiles(a)) {
     // level i: the i-th tiles of all sequences that have it; above(i): the tiles
     // of higher levels.  The number's level is the lowest with above(i) <= tile.
     const int top = (by_key ? s.k_tokens : s.q_tokens) / bt + 1, bits = 32 - __clz(top);
@@ -485,9 +493,14 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int b, int tile, int 
     hit = __ballot(mine > level && below == nth);
     r.tile = by_key ? mine - 1 - level : level;
   } else {
-    r.tile = tile - (by_key ? k0 : q0) / bt - lo - lane;
-    const int starts = __popcll(__ballot(lane < n && r.tile >= 0));
-    hit = starts ? 1ull << (starts - 1) : 0;
+    int upto = mine;  // tiles of this lane's sequence and those before it
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    hit = __ballot(upto > tile);
+    r.tile = tile - (upto - mine);
   }
   const int at = hit ? __ffsll(hit) - 1 : 0;
   r.tile = __builtin_amdgcn_readlane(r.tile, at);
