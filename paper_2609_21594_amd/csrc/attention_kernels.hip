@@ -176,16 +176,16 @@ __device__ __forceinline__ uint2 lds_tr8(uint32_t at) {
 }
 
 // Stages ROWS rows of `dch` chunks, plane by plane, into LDS by direct loads of
-// the whole workgroup of 256.  Rows beyond the sequence repeat its last one and
+// the whole workgroup of NW waves.  Rows beyond the sequence repeat its last one and
 // chunks from dch on the last one: what they hold is finite where the operand
 // is, and meets zeros or is never read.  Load i of a thread has the row of load
 // 0 plus i * STEP; 16 divides STEP, so its chunk is that of load 0, and its
 // 32-bit offset that of load 0 plus a scalar.
-template <int PL, int DU, int ROWS>
+template <int PL, int DU, int ROWS, int NW = 4>
 struct Stager {
   using L = Lay<DU>;
-  static constexpr int STEP = 256 / L::CH, N = ROWS * L::CH / 256;
-  static_assert(ROWS * L::CH % 256 == 0 && STEP % 16 == 0, "whole loads");
+  static constexpr int NT = 64 * NW, STEP = NT / L::CH, N = ROWS * L::CH / NT;
+  static_assert(ROWS * L::CH % NT == 0 && STEP % 16 == 0, "whole loads");
   uint32_t off, stride;
   __device__ __forceinline__ void init(uint32_t stride_, int dch) {
     stride = stride_;
@@ -203,7 +203,7 @@ struct Stager {
 #pragma unroll
         for (int i = 0; i < N; ++i)
           load_lds16(base + p * plane + static_cast<int64_t>(i * STEP) * stride, off,
-                     lds + p * ROWS * L::RB + (i * 256 + wave * 64) * 16);
+                     lds + p * ROWS * L::RB + (i * NT + wave * 64) * 16);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -211,7 +211,7 @@ struct Stager {
                             chunk(dch) * 16;
 #pragma unroll
         for (int p = 0; p < PL; ++p)
-          load_lds16(base + p * plane, at, lds + p * ROWS * L::RB + (i * 256 + wave * 64) * 16);
+          load_lds16(base + p * plane, at, lds + p * ROWS * L::RB + (i * NT + wave * 64) * 16);
       }
     }
   }
@@ -525,7 +525,7 @@ __device__ __forceinline__ void zero_outside(const Seqs& s, bool keys, const Hea
   outside_of(s, keys, lo, hi);
   const int n = keys ? s.k_tokens : s.q_tokens, chunks = bytes / 16;
   const int64_t total = static_cast<int64_t>(lo + n - hi) * chunks;
-  for (int64_t i = threadIdx.x; i < total; i += 256) {
+  for (int64_t i = threadIdx.x; i < total; i += blockDim.x) {
     const int r = static_cast<int>(i / chunks), c = static_cast<int>(i % chunks);
     const int64_t row = r < lo ? r : hi + r - lo;
     *reinterpret_cast<u32x4_t*>(h.p + row * h.token + head * h.head + c * 16) = u32x4_t{0, 0, 0, 0};
@@ -564,18 +564,21 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 // ---------------------------------------------------------------------------
 // Forward.  A wave holds 32 queries and passes over the keys in tiles of BN,
 // staged in LDS (NST stages), keeping the running maximum and sum.  WS = 1: the
-// workgroup's 4 waves hold 128 queries and share each tile.  WS > 1: WS waves
+// workgroup's NW waves hold 32 queries each and share each tile (8 waves: SUB
+// tiles a stage, so that the two waves of a SIMD drift apart between barriers
+// and one has its products while the other has its softmax).  WS > 1: WS waves
 // share their queries and take every WS-th tile, and are joined at the end; for
 // requests with too few rows to fill the device.
 // ---------------------------------------------------------------------------
-template <int PL, int DU, int BN, int WS, int NST, bool FINE, bool SPLIT>
-__global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
+template <int PL, int DU, int BN, int WS, int NST, bool FINE, bool SPLIT, int NW>
+__global__ __launch_bounds__(64 * NW, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
   constexpr int PA = kAccPlanes<PL, FINE>;
   constexpr int PR = PL == 3 ? 6 : 1, PP = PL == 3 ? 6 : PA;  // MFMAs of a product, and of one with an accumulator
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
-  constexpr int BM = 128 / WS, KB = BN / 32, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
-  constexpr int JOIN = (WS - 1) * (4 / WS) * (L::DB * 16 + 3) * 256;
+  constexpr int SUB = NW == 8 ? 2 : 1;  // tiles of a stage, for each wave
+  constexpr int BM = 32 * NW / WS, KB = BN / 32, SR = BN * WS * SUB, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
+  constexpr int JOIN = (WS - 1) * (NW / WS) * (L::DB * 16 + 3) * 256;
   __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE > JOIN ? NST * STAGE : JOIN];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -593,7 +596,7 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
     if (a.res.p) zero_outside(a.seqs, false, a.res, h, a.dim * sizeof(T));
     int lo, hi;
     outside_of(a.seqs, false, lo, hi);
-    for (int i = threadIdx.x; i < lo + a.seqs.q_tokens - hi; i += 256)
+    for (int i = threadIdx.x; i < lo + a.seqs.q_tokens - hi; i += 64 * NW)
       a.lse[row_index(a, 0, h, i < lo ? i : hi + i - lo)] = -kInf;
     return;
   }
@@ -628,7 +631,7 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
 
   const uint32_t lds0 = lds_offset(smem);
   const uint32_t own = lds0 + ws * BN * L::RB, rbase = own + rows_base<DU>(lane), cbase = own + cols_base<DU>(lane);
-  Stager<PL, DU, SR> ks, vs;
+  Stager<PL, DU, SR, NW> ks, vs;
   ks.init(static_cast<uint32_t>(a.sk.token), dch);
   vs.init(static_cast<uint32_t>(a.sv.token), dch);
   const char* const krow = at_row(a.sk, it.b, s.k0, it.kvh);
@@ -655,73 +658,76 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
     wait_loads();
     __syncthreads();  // tile t has landed, and every wave is done with tile t - 1
     if (NST > 1 && t + 1 < t1) issue(t + 1);
-    const int j0 = t * SR + ws * BN;
-    if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
-    const uint32_t rb = rbase + t % NST * STAGE, cb = cbase + t % NST * STAGE;
-    f32x16_t p[KB];
-    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+    for (int sub = 0; sub < SUB; ++sub) {
+      const int j0 = t * SR + (ws + sub) * BN;
+      if (j0 >= wv.end || j0 + BN <= wv.beg) continue;
+      const uint32_t at = t % NST * STAGE + sub * BN * L::RB, rb = rbase + at, cb = cbase + at;
+      f32x16_t p[KB];
+      wave_priority<NW == 8>();
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) p[kb] = zero16();
+      for (int kb = 0; kb < KB; ++kb) p[kb] = zero16();
 #pragma unroll
-    for (int st = 0; st < L::STEPS; ++st)
+      for (int st = 0; st < L::STEPS; ++st)
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * kb * L::RB, st), qf[st], p[kb]);
-    interleave<PR * KB * L::STEPS, PL * KB * L::STEPS, 4>();
-    __builtin_amdgcn_sched_barrier(0);
-    if (j0 + BN > wv.all_end || j0 < wv.all_beg) {
-      asm volatile("; a tile that the mask cuts");  // (a branch: else every tile pays for the comparisons)
-      const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
+        for (int kb = 0; kb < KB; ++kb) mma<PL>(frag_rows<PL, PLANE>(rb, 32 * kb * L::RB, st), qf[st], p[kb]);
+      interleave<PR * KB * L::STEPS, PL * KB * L::STEPS, 4>();
+      wave_priority<0>();
+      if (j0 + BN > wv.all_end || j0 < wv.all_beg) {
+        asm volatile("; a tile that the mask cuts");  // (a branch: else every tile pays for the comparisons)
+        const int lo = jmin - j0 - 4 * half, hi = jmax - j0 - 4 * half;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
+            if (j < lo || j > hi) p[kb][r] = -kInf;
+          }
+      }
+      float mx = -kInf;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[kb][r]);
+      mx = max32(mx);
+      top = fmaxf(top, mx);
+      // Probabilities are taken relative to m, which follows the maximum only
+      // when that has grown by 2^kSlack: binary32 sums have room for the factor,
+      // bf16 rounds relatively, and most tiles leave o as it is.  (The parts of a
+      // split key axis report m as their maximum.)
+      const float mn = mx * a.scale2;
+      if (__any(mn > m + (SPLIT ? 0.f : kSlack))) {
+        const float up = fmaxf(m, mn), alpha = m == up ? 1.f : exp2_(m - up);
+        m = up;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+      }
+      const float mu = m == -kInf ? 0.f : m;
+      float sum = 0.f;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int j = 32 * kb + 8 * (r >> 2) + (r & 3);
-          if (j < lo || j > hi) p[kb][r] = -kInf;
+          p[kb][r] = exp2_(fmaf(p[kb][r], a.scale2, -mu));
+          sum += p[kb][r];
         }
+      l += sum;
+      wave_priority<NW == 8>();
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const Frag<PA> pf = frag_acc<PA>(p[kb], st);
+#pragma unroll
+          for (int db = 0; db < L::DB; ++db)
+            mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * kb * L::RB, st, db), pf, o[db]);
+        }
+      interleave<PP * KB * 2 * L::DB, PL * KB * 4 * L::DB, 8>();
+      wave_priority<0>();
     }
-    float mx = -kInf;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, p[kb][r]);
-    mx = max32(mx);
-    top = fmaxf(top, mx);
-    // Probabilities are taken relative to m, which follows the maximum only
-    // when that has grown by 2^kSlack: binary32 sums have room for the factor,
-    // bf16 rounds relatively, and most tiles leave o as it is.  (The parts of a
-    // split key axis report m as their maximum.)
-    const float mn = mx * a.scale2;
-    if (__any(mn > m + (SPLIT ? 0.f : kSlack))) {
-      const float up = fmaxf(m, mn), alpha = m == up ? 1.f : exp2_(m - up);
-      m = up;
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < L::DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-    }
-    const float mu = m == -kInf ? 0.f : m;
-    float sum = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[kb][r] = exp2_(fmaf(p[kb][r], a.scale2, -mu));
-        sum += p[kb][r];
-      }
-    l += sum;
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const Frag<PA> pf = frag_acc<PA>(p[kb], st);
-#pragma unroll
-        for (int db = 0; db < L::DB; ++db)
-          mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, TILE + 32 * kb * L::RB, st, db), pf, o[db]);
-      }
-    interleave<PP * KB * 2 * L::DB, PL * KB * 4 * L::DB, 8>();
-    __builtin_amdgcn_sched_barrier(0);
   }
 
   l = sum32(l);
@@ -1456,18 +1462,22 @@ hipError_t stage_sources(AttnArgs& a, int dtype, bool backward, hipStream_t st) 
   return hipGetLastError();
 }
 
-template <int PL, int DU, int BN, int WS, int NST, bool FINE = false>
+template <int PL, int DU, int BN, int WS, int NST, bool FINE = false, int NW = 4>
 hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
   const bool pack = packs_heads(a.seqs, a.group);
-  const int64_t tiles = launch_tiles(a, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 128 / WS);
+  const int64_t tiles = launch_tiles(a, int64_t(a.seqs.q_tokens) * (pack ? a.group : 1), 32 * NW / WS);
   const int64_t grid = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles * a.splits;
-  const dim3 g(static_cast<unsigned>(grid)), b(256);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, true>), g, b, 0, st, a, int(tiles), int(pack));
-  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, false>), g, b, 0, st, a, int(tiles), int(pack));
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
+  const dim3 g(static_cast<unsigned>(grid)), b(64 * NW);
+  if (a.splits == 1) {
+    hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, false, NW>), g, b, 0, st, a, int(tiles), int(pack));
+    return hipGetLastError();
+  }
+  if constexpr (NW == 8) return hipErrorInvalidValue;  // (never split)
+  else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, true, NW>), g, b, 0, st, a, int(tiles), int(pack));
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const int64_t rows = a.seqs.batch * a.q_heads * int64_t(a.seqs.q_tokens);
-  hipLaunchKernelGGL((k_attn_join<typename Io<PL>::T>), dim3(static_cast<unsigned>(rows)), b, 0, st, a);
+  hipLaunchKernelGGL((k_attn_join<typename Io<PL>::T>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1508,6 +1518,28 @@ int waves_a_row(const AttnArgs& a, int dtype, int64_t workgroups, int64_t stream
   if (dtype != DT_BF16) return workgroups >= 512 || stream < 96 ? 1 : a.dim <= 64 ? 4 : 2;
   if (workgroups >= 320 || stream < 256) return 1;
   return workgroups < 256 && stream >= 512 ? 4 : 2;
+}
+
+// Whether a forward workgroup has 8 waves, which halves the loads of tiles into
+// LDS and leaves one barrier to 128 keys, but makes waves wait for those that the
+// mask leaves more keys, and a tile of 256 rows out of a short sequence.
+// Measured on an MI355X, 8 waves' time to 4's (workgroups of 8):
+//   no mask, heads of 64 / 128: 0.94 / 0.99 for 8 x 512 tokens (256), 0.90 /
+//     0.94 for 4 x 1024 (256), 0.89 / 0.92 for 4096 (256), - / 0.85 (160), but
+//     1.05 for 64 x 130 (1024), and 11 sequences in 8192: 1.07
+//   causal, heads of 128: 1.07 (256), 0.98 (384) and 0.89 (512) for 4096 tokens,
+//     0.92 for 4 x 2048 (512), 1.0 for 8 x 1024 (512), 1.03 for 32 x 256 (512);
+//     of 64: 1.05 (512), 0.95 (1024), 0.91 for 16 x 2048 (2048), 0.97 for 32 x
+//     1024 (2048); 6 sequences in 16384: 0.97 / 0.97, 40 in 8192: 1.14
+//   causal in a window, heads of 64: 0.89 to 0.95 for windows of 128 to 1024 in
+//     4096 and 8192 tokens (256 and 512), of 96: 0.96, of 128: 0.98 to 1.09; 20
+//     sequences in 16384: 1.04
+bool eight_waves(const AttnArgs& a, int64_t workgroups, int64_t rows) {
+  if (a.seqs.q_off) rows = a.seqs.n_seq ? rows / a.seqs.n_seq : 0;
+  if (rows < (a.seqs.q_off || a.causal ? 2048 : 512)) return false;
+  if (!a.causal) return workgroups >= 160;
+  if (a.window) return workgroups >= 256 && a.dim <= 96;
+  return workgroups >= (a.dim <= 64 ? 1024 : 512);
 }
 
 // Whether probabilities and their gradients are taken in two planes: where the
@@ -1554,14 +1586,16 @@ hipError_t run_attention_forward(AttnArgs a, int dtype, hipStream_t st, LaunchTi
   if (e != hipSuccess) return e;
   const bool pack = packs_heads(a.seqs, a.group);
   const int64_t rows = pack ? int64_t(a.seqs.q_tokens) * a.group : a.seqs.q_tokens;
-  const int ws = waves_a_row(a, dtype, a.seqs.batch * a.kv_heads * (pack ? 1 : a.group) * tiles_of(a.seqs, rows, 128) * a.splits,
-                             a.seqs.k_tokens / a.splits);
+  const int64_t items = a.seqs.batch * a.kv_heads * (pack ? 1 : a.group);
+  const int ws = waves_a_row(a, dtype, items * tiles_of(a.seqs, rows, 128) * a.splits, a.seqs.k_tokens / a.splits);
+  const bool wide = ws == 1 && a.splits == 1 && eight_waves(a, items * tiles_of(a.seqs, rows, 256), rows);
   e = by_width(a.dim, [&](auto w) {
     constexpr int DU = decltype(w)::value;
     if (dtype != DT_BF16) return ws > 1 ? forward_of<3, DU, 32, DU <= 64 ? 4 : 2, 1>(a, st) : forward_of<3, DU, 32, 1, 2>(a, st);
     if (fine_of(a)) return ws == 4 ? forward_of<1, DU, 32, 4, 2, true>(a, st) : forward_of<1, DU, 64, 1, 2, true>(a, st);
     if (ws == 4) return forward_of<1, DU, 32, 4, 2>(a, st);
-    return ws == 2 ? forward_of<1, DU, 32, 2, 2>(a, st) : forward_of<1, DU, 64, 1, 2>(a, st);
+    if (ws == 2) return forward_of<1, DU, 32, 2, 2>(a, st);
+    return wide ? forward_of<1, DU, 64, 1, 2, false, 8>(a, st) : forward_of<1, DU, 64, 1, 2>(a, st);
   });
   const double es = dtype == DT_BF16 ? 2 : 4, b = double(a.seqs.batch);
   if (e == hipSuccess)

@@ -110,3 +110,47 @@ def test_offsets_out_of_order_stay_inside_the_tensors(muon):
                                 dv=given[3][part], **kw)
         for x in given:
             assert (x[:100] == 5).all() and (x[100 + t:] == 5).all()
+
+
+# batch (0: packed, two sequences), queries, keys, query heads, key heads, head size, causal, window: forward
+# workgroups of 8 waves
+EIGHT = [
+    (4, 513, 600, 16, 16, 64, False, 0),
+    (4, 600, 129, 16, 4, 128, False, 0),
+    (4, 520, 257, 16, 8, 96, False, 0),
+    (8, 2050, 300, 8, 8, 128, True, 0),
+    (8, 2050, 2200, 8, 2, 72, True, 0),
+    (16, 2049, 140, 8, 8, 24, True, 0),
+    (4, 2050, 2050, 8, 2, 64, True, 100),
+    (0, 4300, 310, 16, 16, 40, False, 0),
+]
+
+
+@pytest.mark.parametrize("case", EIGHT, ids=str)
+def test_many_rows_and_long_sequences(muon, case):
+    import torch
+    batch, sq, sk, hq, hkv, d, causal, window = case
+    q, k, v, _ = make((max(1, batch), *case[1:]), "bf16", 1.5)
+    kw, rng = dict(causal=causal, window=window), np.random.default_rng(5)
+    if batch:
+        # lengths of 0, of all and others
+        nq, nk = ([0, n] + [int(x) for x in rng.integers(1, n + 1, batch - 2)] for n in (sq, sk))
+        seqs = [(b, 0, n, 0, m) for b, (n, m) in enumerate(zip(nq, nk))]
+        kw.update((n, torch.tensor(x, dtype=torch.int32, device="cuda")) for n, x in (("q_lens", nq), ("k_lens", nk)))
+    else:
+        seqs = [(0, 3, 2000, 0, 300), (0, 2003, sq - 2003, 300, 5)]
+        kw.update((n, torch.tensor(x, dtype=torch.int32, device="cuda")) for n, x in (("q_offsets", [3, 2003, sq]),
+                                                                                 ("k_offsets", [0, 300, 305])))
+    want = ref.attention(*map(to_host, (q, k, v)), "bf16", causal=causal, window=window, seqs=seqs)
+    if not batch:
+        q, k, v = q[0], k[0], v[0]
+    top, res = torch.full((hq,), -INF, device="cuda"), torch.full_like(q, NAN)
+    out, lse = muon.attention(q, k, v, max_logits=top, residual=res, **kw)
+    close(out, want["out"], "out")
+    close(lse, want["lse"], "lse")
+    close(top, want["top"], "top")
+    r, o = to_host(res), to_host(out)
+    held = np.s_[:] if batch else np.s_[3:]
+    assert (np.abs(r) <= ref.HALF_STEP["bf16"] * np.abs(o + r) * (1 + 2.0 ** -7))[held].all()
+    again, lse2 = muon.attention(q, k, v, **kw)
+    assert np.array_equal(to_bits(again), to_bits(out)) and np.array_equal(to_bits(lse2), to_bits(lse))
