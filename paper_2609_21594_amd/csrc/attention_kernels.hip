@@ -1504,20 +1504,38 @@ hipError_t dkv_of(const AttnArgs& a, hipStream_t st) {
 
 // How many waves share their rows (WS in the kernels): more than one where
 // workgroups of 128 rows would leave compute units idle and a row has enough to
-// pass over.  Measured on an MI355X, WS = 1 / 2 / 4, us:
-//   bf16, 48 workgroups, 512 keys of 64:       11.0 / 10.4 /  7.8 (gradients 31.9 / 24.9 / 20.4)
-//         128, 4096 keys of 128:               74.4 / 61.3 / 49.3 (276 / 205 / 152)
-//         128, a window of 256 in 2000:        13.5 / 11.2 / 20.1 (40 / 32 / 56)
-//         256, 4096 keys of 128:               78.1 / 66.5 / 95.9 (273 / 225 / 285)
-//         384, 700 keys of 96:                 17.8 / 20.8 / 46.5 (59 / 77 / 141)
-//   fp32 (4 where the head has up to 64 elements, else 2; one stage in LDS):
-//         32, 129 keys of 64 (gradients):      42.4 / - / 34.0
-//         256, 1024 keys of 128:               99.4 / 89.3 / - (338 / 249 / -)
+// pass over, as long as the device holds all of them at once (256 workgroups of
+// heads of more than 64 elements, 512 of narrower ones; a causal pass ends half
+// or a third of them early).  Measured on an MI355X, WS = 1 / 2 / 4, us forward
+// (gradients), 4096 tokens unless said otherwise:
+//   heads of 128, no mask:  64 workgroups 76 / 63 / 42 (266 / 199 / 134), 128:
+//     76 / 64 / 83 (273 / 204 / 258), 160: 78 / 84 / 131 (275 / 393 / 391)
+//   causal: 128: 77 / 63 / 50 (270 / 201 / 157), 256: 78 / 69 / 97 (274 / 226 /
+//     297), 384: 83 / 79 / 153 (288 / 357 / 454)
+//   heads of 64, no mask: 128: 56 / 50 / 36 (173 / 131 / 106), 160: 57 / 58 / 59
+//     (177 / 151 / 172), 256: 56 / 60 / 68 (177 / 165 / 198), 288: 81 / 77 / 89
+//     (221 / 245 / 266)
+//   causal: 192: 56 / 49 / 34 (174 / 135 / 98), 256: 57 / 49 / 41 (176 / 137 /
+//     121), 384: 59 / 51 / 58 (184 / 149 / 173), 512: 61 / 58 / 75 (192 / 174 /
+//     221), 512 of 1024 tokens: 20 / 23 / 34 (60 / 65 / 96)
+//   windows of 1024, heads of 128, 384: 44 / 66 / 106 (125 / 196 / 296)
+//   fp32, 1024 tokens, WS = 1 / 2 (more than 64 elements) or 4 (one stage in LDS):
+//     128, no mask, 128: 93 / 70 (313 / 196), 192: 95 / 127 (322 / 360); causal,
+//     256: 96 / 84 (329 / 231), 320: 100 / 112 (344 / 323)
+//     64, no mask, 128: 55 / 55 (159 / 140), 192: 57 / 77 (164 / 205); causal,
+//     192: 57 / 56 (162 / 141), 256: 57 / 69 (166 / 180); 144 of 128 tokens:
+//     21 / 32 (48 / 75)
 int waves_a_row(const AttnArgs& a, int dtype, int64_t workgroups, int64_t stream) {
-  if (a.causal && a.window) stream = std::min<int64_t>(stream, int64_t(a.window) + 128);
-  if (dtype != DT_BF16) return workgroups >= 512 || stream < 96 ? 1 : a.dim <= 64 ? 4 : 2;
-  if (workgroups >= 320 || stream < 256) return 1;
-  return workgroups < 256 && stream >= 512 ? 4 : 2;
+  const bool window = a.causal && a.window, narrow = a.dim <= 64;
+  if (window) stream = std::min<int64_t>(stream, int64_t(a.window) + 128);
+  const int64_t whole = workgroups, slots = narrow ? 512 : 256;
+  if (a.causal && !window && stream >= 512) workgroups = narrow ? workgroups * 2 / 3 : workgroups / 2;
+  if (dtype != DT_BF16) {
+    const int ws = narrow ? 4 : 2;
+    return stream >= 512 ? (workgroups * ws <= slots ? ws : 1) : stream >= 96 && whole * ws <= 256 ? ws : 1;
+  }
+  if (stream >= 512 && workgroups * 4 <= slots) return 4;
+  return stream >= 256 && workgroups * 2 <= slots ? 2 : 1;
 }
 
 // Whether a forward workgroup has 8 waves, which halves the loads of tiles into

@@ -22,6 +22,7 @@ SIZES = [
     ("bf16", 4, 300, 301, 4, 2, 64, True, 0),       # 48, over 301 keys
     ("bf16", 4, 300, 301, 4, 4, 128, False, 0),
     ("bf16", 9, 400, 260, 8, 8, 24, True, 0),       # 288
+    ("bf16", 5, 500, 490, 4, 4, 96, True, 0),       # 80, over 490
     ("bf16", 2, 600, 700, 4, 2, 64, True, 0),       # 40, over 700
     ("bf16", 2, 600, 700, 4, 1, 96, True, 0),
     ("bf16", 2, 533, 520, 4, 2, 128, False, 0),
