@@ -175,7 +175,7 @@ ScratchPlan plan_scratch(const muon_attention_t* a, bool backward) {
   } else {
     take(p.lse2, size_t(rows) * 4);
     take(p.delta, size_t(rows) * 4);
-    p.kv_parts = muon::backward_parts(s, a->q_heads, a->kv_heads);
+    p.kv_parts = muon::backward_parts(s, a->q_heads, a->kv_heads, a->causal != 0, window_of(a));
     if (p.kv_parts > 1) {
       take(p.dk, size_t(keys) * size_t(p.kv_parts) * size_t(a->head_dim) * 4);
       take(p.dv, size_t(keys) * size_t(p.kv_parts) * size_t(a->head_dim) * 4);

@@ -65,7 +65,7 @@ hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchT
 // spread (1: none), and in how many parts its backward pass takes the query
 // heads that share keys.
 int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window);
-int backward_parts(const Seqs& s, int q_heads, int kv_heads);
+int backward_parts(const Seqs& s, int q_heads, int kv_heads, bool causal, int window);
 
 constexpr int kRotaryMax = 4;
 struct RotaryTensor {

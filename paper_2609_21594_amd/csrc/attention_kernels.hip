@@ -1589,11 +1589,25 @@ int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int wi
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
 }
 
-int backward_parts(const Seqs& s, int q_heads, int kv_heads) {
+// The smallest number of parts that gives the device enough workgroups: parts
+// cost fp32 gradients written and added up, too few workgroups leave compute
+// units idle, most in a long causal pass, whose first keys take longest.
+// Measured on an MI355X, groups of 4, 1 / 2 / 4 parts, us (workgroups of 1 part):
+//   causal, 4096 tokens x 8 heads of 128: 657 / 567 / 481 (256); 2 of them: 1065
+//     / 915 / 957 (512); 4: 1722 / 1794 / 1905 (1024); 4 x 2048: 562 / 512 / 577
+//     (512); 8 x 1024: 321 / 333 / 400 (512); 4 x 1024: 197 / 185 / 188 (256);
+//     8 x 512: 127 / 124 / 145 (256); 4 x 512: 88 / 87 / 77 (128); 32 x 128: 77 /
+//     85 / 114 (256); 16 x 128, heads of 64: 27 / 34 / 38 (128)
+//   a window of 1024 in 8192: 474 / 519 / 575 (512); of 512 in 4096: 181 / 170 /
+//     195 (256); no mask, 4096: 987 / 845 / 866 (256), 4 x 2048: 833 / 885 / 955
+//     (512), 2048: 311 / 273 / 242 (128)
+int backward_parts(const Seqs& s, int q_heads, int kv_heads, bool causal, int window) {
   const int group = q_heads / kv_heads;
   const int64_t items = s.batch * kv_heads * tiles_of(s, s.k_tokens, 128);
+  const int64_t length = s.q_off ? s.k_tokens / std::max(1, s.n_seq) : s.k_tokens;
+  const int64_t enough = length <= 128 ? 128 : length >= 2048 && causal && !window ? 1024 : 512;
   for (int p = 1; p < group; ++p)
-    if (group % p == 0 && items * p >= 1024) return p;
+    if (group % p == 0 && items * p >= enough) return p;
   return group;
 }
 

@@ -30,6 +30,9 @@ SIZES = [
     ("bf16", 2, 4097, 1, 1, 1, 16, False, 0),       # one key
     # the heads of a group: each by itself, two parts, all at once
     ("bf16", 32, 33, 130, 32, 8, 16, True, 0),
+    ("bf16", 16, 33, 130, 32, 8, 16, True, 0),
+    ("f32", 16, 33, 130, 32, 8, 24, True, 20),
+    ("bf16", 8, 600, 128, 16, 4, 128, False, 0),
     ("bf16", 64, 40, 130, 16, 8, 16, True, 0),
     ("f32", 32, 33, 130, 32, 8, 16, True, 0),
     ("f32", 64, 40, 130, 16, 8, 16, False, 0),
