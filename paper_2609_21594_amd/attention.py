@@ -120,7 +120,11 @@ def rotary(lib, xs, freqs, positions=None, first=0, layout="half", scale=1.0, in
     """`Muon.rotary` with gradients: a tensor, or a list of up to 4."""
     one = torch.is_tensor(xs)
     xs = [xs] if one else list(xs)
-    ys = _Rotary.apply(lib, freqs, positions, dict(first=first, layout=layout, scale=scale, inverse=inverse), *xs)
+    kw = dict(first=first, layout=layout, scale=scale, inverse=inverse)
+    if torch.is_grad_enabled():
+        ys = _Rotary.apply(lib, freqs, positions, kw, *xs)
+    else:
+        ys = lib.rotary(xs, freqs, positions=positions, **kw)
     return ys[0] if one else list(ys)
 
 
@@ -157,7 +161,10 @@ def attention(lib, q, k, v, scale=None, causal=False, window=0, q_offsets=None, 
               k_lens=None, max_logits=None, return_lse=False):
     """`Muon.attention` with gradients for q, k and v (lse and max_logits carry
     none).  bf16 outputs keep what their rounding took for the backward pass."""
-    out, lse = _Attention.apply(lib, q, k, v, max_logits,
-                                dict(scale=scale, causal=causal, window=window, q_offsets=q_offsets,
-                                     k_offsets=k_offsets, q_lens=q_lens, k_lens=k_lens))
+    kw = dict(scale=scale, causal=causal, window=window, q_offsets=q_offsets, k_offsets=k_offsets, q_lens=q_lens,
+              k_lens=k_lens)
+    if torch.is_grad_enabled():
+        out, lse = _Attention.apply(lib, q, k, v, max_logits, kw)
+    else:
+        out, lse = lib.attention(q, k, v, max_logits=max_logits, **kw)
     return (out, lse) if return_lse else out

@@ -447,11 +447,15 @@ def _expect(t, shape, dtype, what):
 
 
 def clip_records(wqs, wks, max_logits, threshold) -> bytes:
-    """Packed entries of muon_qk_clip, their shapes checked (host only)."""
+    """Packed entries of muon_qk_clip, their shapes checked (host only).
+    threshold: a number, or one of each entry."""
     import torch
     codes, f32 = {torch.float32: F32, torch.bfloat16: BF16}, torch.float32
-    threshold, pack, recs = float(threshold), _CLIP_PACK.pack, []
-    for i, (q, k, m) in enumerate(zip(wqs, wks, max_logits)):
+    each = [float(t) for t in threshold] if isinstance(threshold, (list, tuple)) else [float(threshold)] * len(wqs)
+    if len(each) != len(wqs):
+        raise ValueError("one threshold, or one of each entry")
+    pack, recs = _CLIP_PACK.pack, []
+    for i, (q, k, m, threshold) in enumerate(zip(wqs, wks, max_logits, each)):
         qs, ks, hq = q.shape, k.shape, m.numel()
         if len(qs) != 2 or len(ks) != 2 or qs[1] != ks[1] or q.dtype is not k.dtype:
             raise ValueError(f"entry {i}: weights must be matrices of one dtype and one number of columns")
@@ -781,8 +785,9 @@ class Muon:
     def qk_clip(self, wqs, wks, max_logits, threshold, reset=False, stream=None):
         """In place: scales the rows of query weights wqs[i] [Hq * hd, cols] and
         key weights wks[i] [Hkv * hd, cols] so that every head whose largest
-        logit max_logits[i] (fp32, [Hq]) exceeds `threshold` comes down to it
-        (muon_qk_clip).  reset: the logits become -inf afterwards."""
+        logit max_logits[i] (fp32, [Hq]) exceeds `threshold` (a number, or a
+        list of one for each entry) comes down to it (muon_qk_clip).  reset:
+        the logits become -inf afterwards."""
         n = len(wqs)
         if not (len(wks) == len(max_logits) == n):
             raise ValueError("query weights, key weights and logits must have equal length")

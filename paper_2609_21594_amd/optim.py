@@ -74,7 +74,7 @@ class MuonAdamW(torch.optim.Optimizer):
         if any(w.untyped_storage().data_ptr() not in params for w in entry[:2]):
             raise ValueError("wq and wk must be parameters of this optimizer, or views of them")
         # (with the earlier ones: no weight is clipped twice)
-        validate_qk_clip(*zip(*[c[:3] for c in self._clips + [entry]]), entry[3])
+        validate_qk_clip(*zip(*self._clips, entry))
         self._clips.append(entry)
 
     def load_state_dict(self, state_dict):
@@ -143,7 +143,6 @@ class MuonAdamW(torch.optim.Optimizer):
                                      [ms[i] for i in idx], [vs[i] for i in idx], t,
                                      lr=group["adamw_lr"], betas=tuple(group["adamw_betas"]),
                                      eps=group["adamw_eps"], weight_decay=group["adamw_weight_decay"])
-        for threshold in dict.fromkeys(c[3] for c in self._clips):  # one call per threshold
-            wqs, wks, logits, _ = zip(*(c for c in self._clips if c[3] == threshold))
-            self._lib.qk_clip(wqs, wks, logits, threshold, reset=True)
+        if self._clips:
+            self._lib.qk_clip(*zip(*self._clips), reset=True)
         return loss

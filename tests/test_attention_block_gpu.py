@@ -209,6 +209,23 @@ def test_block_gradients_and_training_step(muon):
     opt.close()
 
 
+def test_weights_that_share_logits_are_clipped_by_thresholds_of_their_own(muon):
+    import torch
+    from paper_2609_21594_amd.optim import MuonAdamW
+    ws = [torch.nn.Parameter(torch.ones(16, 24, device="cuda")) for _ in range(4)]
+    top = torch.tensor([8.0, 1.0], device="cuda")
+    opt = MuonAdamW(ws, lr=0.0, adamw_lr=0.0)
+    opt.clip_query_keys(ws[0], ws[1], top, 2.0)
+    opt.clip_query_keys(ws[2], ws[3], top, 4.0)
+    opt.step()
+    # factors 2 / 8 and 4 / 8 of head 0, their square roots to queries and keys:
+    # 0.5 is exact, 0.5 ** 0.5 off by at most one rounding of the root and one of the product
+    for w, f in zip(ws, (0.5, 0.5, 0.5 ** 0.5, 0.5 ** 0.5)):
+        assert ((w[:8] - f).abs() <= 2 * 2.0 ** -24).all() and (w[8:] == 1).all()
+    assert torch.isneginf(top).all()
+    opt.close()
+
+
 def test_gradients_against_differences(muon):
     import torch
     from paper_2609_21594_amd.attention import attention, rotary, rotary_frequencies
@@ -376,3 +393,27 @@ def test_profile_names_the_calls(muon):
     assert got["attention_forward"]["launches"] == 1 and got["attention_backward"]["launches"] == 1
     assert got["attention_forward"]["total_ms"] > 0 and got["rotary"]["launches"] == 0
     del torch
+
+
+def test_inference_is_captured_beside_an_eager_graph(muon):
+    """Without gradients there is nothing to accumulate, so nothing to refuse."""
+    import torch
+    from paper_2609_21594_amd.attention import attention, rotary, rotary_frequencies
+    q, k, v = (torch.randn(1, 20, 2, 16, device="cuda", dtype=torch.bfloat16, requires_grad=True) for _ in range(3))
+    freqs = rotary_frequencies(16).cuda()
+
+    def run():
+        return attention(muon, *rotary(muon, [q, k], freqs), v, causal=True)
+    eager = run()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.no_grad(), torch.cuda.graph(graph):
+        out = run()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(to_bits(out), to_bits(eager.detach()))
+    assert not out.requires_grad
+    eager.sum().backward()
+    assert torch.isfinite(q.grad).all()
