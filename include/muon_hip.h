@@ -42,7 +42,8 @@
  *     an error other than MUON_ERR_DEVICE changed nothing.  Values inside the
  *     tensors are never checked; NaN and Inf propagate.  The calls that
  *     launch work (muon_step, ns_orthogonalize_batched, muon_adamw_step, the
- *     attention block's) also ask the runtime about every buffer: it must start in device memory of
+ *     attention block's) also ask the runtime about every buffer: it must start
+ *     in device memory of
  *     the handle's device (or managed memory), and if it reaches beyond the
  *     allocation that holds its start, its last byte must be such memory too
  *     (allocations mapped back to back); otherwise MUON_ERR_INVALID_ARGUMENT.  muon_validate_step does not query the
@@ -332,8 +333,7 @@ typedef struct {
  * inputs hold.  Packed: batch = 1, and q_offsets and k_offsets (device, int32,
  * [sequences + 1], not decreasing, both or neither) cut the token axes into
  * sequences; rows outside every sequence are left as they are (or see
- * fill_rest).  Lengths and
- * offsets beyond the axes are cut to them.
+ * fill_rest).  Lengths and offsets beyond the axes are cut to them.
  *
  * Inputs that are not finite propagate; one that only some queries of a
  * sequence may see can also reach the others (0 * inf).
@@ -418,8 +418,8 @@ muon_status_t muon_validate_rotary(const muon_rotary_t* r, const muon_rotary_ten
 
 /* QK-clip of n pairs of weights.  wq is [q_heads * head_dim][cols], wk
  * [kv_heads * head_dim][cols], row strides q_ld and k_ld (elements, 0 = cols).
- * With M_h = max_logits[h], g_h = min(1, threshold / M_h) where M_h > threshold
- * (1 otherwise and where M_h is not finite) and G = min g_h over the query
+ * With M_h = max_logits[h], g_h = threshold / M_h (2^-126 at least) where M_h >
+ * threshold (1 otherwise and where M_h is not finite) and G = min g_h over the query
  * heads that share a key head:
  *   wk (its rows) *= sqrt(G)        wq (rows of h) *= g_h / sqrt(G)
  * so that head h's logits scale by g_h.  Rows whose factor is 1 are not

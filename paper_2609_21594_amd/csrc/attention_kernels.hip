@@ -1347,7 +1347,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int per_block) {
 // are not touched.  HBM-bound on the rows that change.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float clip_gamma(float m, float threshold) {
-  return m > threshold && m < kInf ? threshold / m : 1.f;
+  return m > threshold && m < kInf ? fmaxf(threshold / m, 0x1p-126f) : 1.f;  // (0 would have no root to divide by)
 }
 template <typename T>
 __global__ __launch_bounds__(256) void k_qk_clip(ClipArgs a) {

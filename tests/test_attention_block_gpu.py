@@ -209,6 +209,17 @@ def test_block_gradients_and_training_step(muon):
     opt.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_qk_clip_of_factors_below_binary32(muon, dtype):
+    """1e-30 / 1e20 has no binary32 value; the weights stay numbers."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    wq, wk = torch.ones(16, 8, device="cuda", dtype=t), torch.ones(8, 8, device="cuda", dtype=t)
+    muon.qk_clip([wq], [wk], [torch.tensor([1e20, 1e-31], device="cuda")], 1e-30)
+    # 2^-126 split as 2^-63 and 2^-63, exact; the other head keeps its logits
+    assert (wk == 2.0 ** -63).all() and (wq[:8] == 2.0 ** -63).all() and (wq[8:] == 2.0 ** 63).all()
+
+
 def test_weights_that_share_logits_are_clipped_by_thresholds_of_their_own(muon):
     import torch
     from paper_2609_21594_amd.optim import MuonAdamW
