@@ -11,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
@@ -27,26 +28,44 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found: the HIP library cannot be built")
 
 
-def command(out: str = LIB):
-    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
-            "-Wall", "-Wno-unused-function",
-            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            "-I", os.path.join(ROOT, "include"),
-            *[os.path.join(HERE, s) for s in SOURCES], "-o", out]
+def commands(out: str, objects: str):
+    """One command for each source, and the one that links their objects."""
+    flags = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include")]
+    objs = [os.path.join(objects, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+    return ([[*flags, "-c", os.path.join(HERE, s), "-o", o] for s, o in zip(SOURCES, objs)],
+            [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", *objs, "-o", out])
 
 
 def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
-    cmd = command(tmp)
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+
+    def finish(cmd, run):
+        _, err = run.communicate()
+        err = "\n".join(l for l in err.splitlines() if noise not in l)
+        if run.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({run.returncode}): {' '.join(cmd)}\n{err}")
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    def start(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
+
+    with tempfile.TemporaryDirectory() as objects:
+        compiles, link = commands(tmp, objects)
+        runs = [start(c) for c in compiles]  # at once: the kernels take minutes one after the other
+        try:
+            for c, r in zip(compiles, runs):
+                finish(c, r)
+        finally:
+            for r in runs:
+                if r.poll() is None:
+                    r.kill()
+                    r.wait()
+        finish(link, start(link))
     os.replace(tmp, LIB)
     return LIB
 
