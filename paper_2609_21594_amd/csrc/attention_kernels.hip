@@ -1361,7 +1361,7 @@ __global__ __launch_bounds__(256) void k_qk_clip(ClipArgs a) {
   const int rows_q = e.q_heads * e.dim, rows = rows_q + e.kv_heads * e.dim;
   const int base = (blockIdx.x - a.first[k]) * a.rows;
   bool any = false;
-  if (threadIdx.x < a.rows) {
+  if (static_cast<int>(threadIdx.x) < a.rows) {
     const int row = base + threadIdx.x;
     float f = 1.f;
     if (row < rows) {
@@ -1472,7 +1472,9 @@ hipError_t forward_of(const AttnArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, false, NW>), g, b, 0, st, a, int(tiles), int(pack));
     return hipGetLastError();
   }
-  if constexpr (NW == 8) return hipErrorInvalidValue;  // (never split)
+  // split passes are of few queries: no 8 waves, and rows beyond fine_of's are so
+  // many heads that their parts are many workgroups too
+  if constexpr (NW == 8 || (PL == 1 && WS == 4 && !FINE)) return hipErrorInvalidValue;
   else hipLaunchKernelGGL((k_attn_fwd<PL, DU, BN, WS, NST, FINE, true, NW>), g, b, 0, st, a, int(tiles), int(pack));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
