@@ -167,7 +167,7 @@ ScratchPlan plan_scratch(const muon_attention_t* a, bool backward) {
   const auto take = [&](size_t& at, size_t bytes) { at = p.bytes; p.bytes += up256(bytes); };
   if (rows == 0 && (!backward || keys == 0)) return p;
   if (!backward) {
-    p.splits = muon::forward_splits(s, a->q_heads, a->kv_heads, a->causal != 0, window_of(a));
+    p.splits = muon::forward_splits(s, a->q_heads, a->kv_heads, a->head_dim, a->causal != 0, window_of(a));
     if (p.splits > 1) {
       take(p.part_o, size_t(rows) * size_t(p.splits) * size_t(a->head_dim) * 4);
       take(p.part_ml, size_t(rows) * size_t(p.splits) * 8);

@@ -64,7 +64,7 @@ hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchT
 // Over how many parts of the key axis the forward pass of this request is
 // spread (1: none), and in how many parts its backward pass takes the query
 // heads that share keys.
-int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window);
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, bool causal, int window);
 int backward_parts(const Seqs& s, int q_heads, int kv_heads, bool causal, int window);
 
 constexpr int kRotaryMax = 4;

@@ -1581,12 +1581,22 @@ hipError_t by_width(int dim, F&& f) {
 
 }  // namespace
 
-int forward_splits(const Seqs& s, int q_heads, int kv_heads, bool causal, int window) {
-  if (s.q_off || (causal && window) || s.q_tokens > 128) return 1;
-  const bool pack = packs_heads(s, q_heads / kv_heads);
+// A single pass where its workgroups fill the device or its keys are few; else
+// parts of at least four tiles each, for two workgroups a CU.  Measured on an
+// MI355X, one part / these, us:
+//   one token, 32 heads on 8 of 128: 32 x 4096 keys 119 / 115 (2 parts); 16 heads
+//     of 64, 16 x 4096: 78 / 48 (2); 32 x 1024: 29 / 30 (2)
+//   more than 128 queries, heads of 128 (waves sharing rows / these): 512 on 8192
+//     keys, 32 heads 159 / 97 (4 parts), on 4096 80 / 62, on 2048 45 / 46; 256 on
+//     3000 34 / 37; 1024 on 4096, 16 heads 75 / 63; 4096 on 4096, 4 heads 54 / 60;
+//     200 on 2 x 8192 167 / 92; of 64: 512 on 8192, 16 heads 51 / 42, on 4096, 8
+//     heads 32 / 26; 1024 on 4096, 8 heads 28 / 34; 4 x 256 on 4096, 16 heads 41 / 50
+int forward_splits(const Seqs& s, int q_heads, int kv_heads, int dim, bool causal, int window) {
+  if (s.q_off || (causal && window)) return 1;
+  const bool many = s.q_tokens > 128, pack = packs_heads(s, q_heads / kv_heads);
+  if (many && (s.k_tokens < 4096 || s.k_tokens / s.q_tokens < (dim <= 64 ? 8 : 4))) return 1;
   const int64_t items = s.batch * (pack ? int64_t(kv_heads) : q_heads * tiles_of(s, s.q_tokens, 128));
-  if (items == 0 || items >= 256) return 1;
-  // four tiles of keys at least in each part
+  if (items == 0 || items > (!many ? 256 : dim <= 64 ? 64 : 255)) return 1;
   const int64_t parts = std::min<int64_t>(512 / items, s.k_tokens / 256);
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
 }

@@ -116,6 +116,44 @@ def test_offsets_out_of_order_stay_inside_the_tensors(muon):
             assert (x[:100] == 5).all() and (x[100 + t:] == 5).all()
 
 
+# few rows of many heads, or more than 128 queries, on a long key axis in parts
+PARTS = [
+    ("bf16", 16, 1, 600, 16, 16, 64, True, 0),      # 256 workgroups
+    ("bf16", 32, 2, 520, 32, 8, 96, True, 0),
+    ("bf16", 1, 200, 4100, 8, 2, 128, True, 0),
+    ("bf16", 1, 515, 4121, 12, 12, 40, False, 0),
+    ("bf16", 1, 1030, 4200, 4, 1, 128, True, 0),
+    ("bf16", 5, 129, 4096, 4, 4, 72, True, 0),
+    ("f32", 1, 200, 4100, 4, 2, 128, True, 0),
+    ("f32", 2, 300, 4096, 3, 3, 64, False, 0),
+]
+
+
+@pytest.mark.parametrize("case", PARTS, ids=str)
+@pytest.mark.parametrize("padded", [False, True])
+def test_parts_of_the_keys(muon, case, padded):
+    import torch
+    dtype, case = case[0], case[1:]
+    b, sq, sk, hq, _, _, causal, _ = case
+    q, k, v, _ = make(case, dtype, 1.5)
+    kw, seqs = dict(causal=causal), None
+    if padded:  # lengths that leave parts, and whole sequences, without a key
+        nq = [sq, 0, 1, sq - sq // 3, sq, 3][:b] + [sq] * (b - 6)
+        nk = [sk - 300, 40, sk, sk // 2, 0, 17][:b] + [sk - 1] * (b - 6)
+        seqs = [(i, 0, min(n, sq), 0, m) for i, (n, m) in enumerate(zip(nq, nk))]  # (the kernels cut them too)
+        kw.update((n, torch.tensor(x, dtype=torch.int32, device="cuda")) for n, x in (("q_lens", nq), ("k_lens", nk)))
+    want = ref.attention(*map(to_host, (q, k, v)), dtype, causal=causal, seqs=seqs)
+    top = torch.full((hq,), -INF, device="cuda")
+    res = torch.full_like(q, NAN) if dtype == "bf16" else None
+    out, lse = muon.attention(q, k, v, max_logits=top, residual=res, **kw)
+    close(out, want["out"], "out")
+    close(lse, want["lse"], "lse")
+    close(top, want["top"], "top")
+    if res is not None:
+        r, o = to_host(res), to_host(out)
+        assert (np.abs(r) <= ref.HALF_STEP["bf16"] * np.abs(o + r) * (1 + 2.0 ** -7)).all()
+
+
 # batch (0: packed, two sequences), queries, keys, query heads, key heads, head size, causal, window: forward
 # workgroups of 8 waves
 EIGHT = [
