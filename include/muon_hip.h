@@ -381,7 +381,11 @@ muon_status_t muon_validate_attention(const muon_attention_t* a, const muon_atte
 muon_status_t muon_attention_forward(muon_handle_t h, const muon_attention_t* a, void* stream);
 /* Writes dq, dk and dv from q, k, v, out, residual, lse and dout; the
  * probabilities are recomputed.  Key and value gradients are summed over the
- * query heads that share them.  Deterministic: no floating-point atomics. */
+ * query heads that share them.  Deterministic: no floating-point atomics.
+ * lse and out may be those of a softmax over more keys than these: dk and dv
+ * are then these keys' gradients, and dq their part of it.  (fp32: a row whose
+ * probabilities sum to 1 within the rounding of lse, 2^-22 (|lse| log2(e) + 8),
+ * is taken to sum to 1.) */
 muon_status_t muon_attention_backward(muon_handle_t h, const muon_attention_t* a, const muon_attention_grad_t* g,
                                       void* stream);
 

@@ -157,7 +157,7 @@ int32_t window_of(const muon_attention_t* a) {  // one beyond every gap is none
 
 struct ScratchPlan {
   int splits = 1, kv_parts = 1;
-  size_t part_o = 0, part_ml = 0, lse2 = 0, delta = 0, dk = 0, dv = 0;
+  size_t part_o = 0, part_ml = 0, lse2 = 0, delta = 0, norm = 0, dk = 0, dv = 0;
   size_t sq = 0, sk = 0, sv = 0, sdo = 0, bytes = 0;
 };
 ScratchPlan plan_scratch(const muon_attention_t* a, bool backward) {
@@ -175,6 +175,7 @@ ScratchPlan plan_scratch(const muon_attention_t* a, bool backward) {
   } else {
     take(p.lse2, size_t(rows) * 4);
     take(p.delta, size_t(rows) * 4);
+    if (a->dtype == MUON_F32) take(p.norm, size_t(rows) * 4);
     p.kv_parts = muon::backward_parts(s, a->q_heads, a->kv_heads, a->causal != 0, window_of(a));
     if (p.kv_parts > 1) {
       take(p.dk, size_t(keys) * size_t(p.kv_parts) * size_t(a->head_dim) * 4);
@@ -280,6 +281,7 @@ muon_status_t check_attention(const muon_attention_t* a, const muon_attention_gr
   if (g) {
     k.lse2 = part(p.lse2);
     k.delta = part(p.delta);
+    if (a->dtype == MUON_F32) k.norm = part(p.norm);
     if (p.kv_parts > 1) { k.part_dk = part(p.dk); k.part_dv = part(p.dv); }
   }
   if (a->dtype == MUON_F32) {

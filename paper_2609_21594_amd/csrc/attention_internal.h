@@ -41,9 +41,9 @@ struct AttnArgs {
   int32_t splits;
   float* part_o;             // [splits][rows][dim]
   float2* part_ml;           // [splits][rows]
-  // backward: per row log2(sum exp) (+inf where nothing is visible) and
-  // dout . out
-  float *lse2, *delta;
+  // backward: per row log2(sum exp) (+inf where nothing is visible), dout . out,
+  // and (fp32) what the probabilities are multiplied with
+  float *lse2, *delta, *norm;
   // backward, the heads of a group in kv_parts parts with workgroups of their
   // own: where more than one, the parts' fp32 gradients,
   // [batch * k_tokens][kv_heads][kv_parts][dim]

@@ -891,6 +891,19 @@ __device__ __forceinline__ bool join_waves(f32x16_t* acc, char* smem, int wave, 
   return true;
 }
 
+// fp32: what a row's probabilities are multiplied with, 0: they stay.  lse2 holds
+// the log-sum-exp to half a step of its own size, 2^-24 |lse2|, twice (as lse, and
+// times log2 e), which all probabilities of the row have as a common factor: at
+// |lse2| = 72 up to 5e-6 of the gradients, ten times their other errors.  Their
+// own sum tells the factor.  A sum further from 1 than such roundings is what lse
+// says (it may be that of more keys).  Rows so normalised also know what their
+// dS should sum to, which takes the rounding of out from delta.  Measured, errors
+// of dq and dk with logits of size 16 to 45: 0.4 to 1.1e-6 instead of 1.2 to
+// 2.7e-6, for 4% more time.
+__device__ __forceinline__ float row_norm(float total, float lse2) {
+  return total > 0.5f && fabsf(total - 1.f) <= 0x1p-22f * (fabsf(lse2) + 8.f) ? 1.f / total : 0.f;
+}
+
 // dout . (out + res) of the lane's row, as the diagonal of the products of 32
 // rows of out with those of dout: the same operation, in the same order, as
 // that of dout with a value row.  A row that sees one key has out equal to it
@@ -926,8 +939,8 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
   constexpr int BM = 128 / WS, SR = BN * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
-  constexpr int JOIN = (WS - 1) * (4 / WS) * L::DB * 4096;
-  __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE > JOIN ? NST * STAGE : JOIN];
+  constexpr int JOIN = (WS - 1) * (4 / WS) * L::DB * 4096, USED = JOIN + (PL == 3 && WS > 1 ? 2048 : 0);
+  __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE > USED ? NST * STAGE : USED];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ws = wave % WS, dch = (a.dim + 7) / 8;
@@ -979,6 +992,13 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
   f32x16_t acc[L::DB];
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
+  // fp32: the sums of the row's probabilities and of dS, and sum_j p_j k_j to bf16's accuracy
+  float total = 0.f, rest = 0.f;
+  f32x16_t pk[PL == 3 ? L::DB : 1];
+  if constexpr (PL == 3) {
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db) pk[db] = zero16();
+  }
   for (int t = t0; t < t1; ++t) {
     if constexpr (NST == 1) {
       __syncthreads();
@@ -1010,31 +1030,78 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
         }
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) d[e] = exp2_(fmaf(p[e], a.scale2, -lse2)) * (d[e] - delta);
+      for (int e = 0; e < 16; ++e) {
+        const float x = exp2_(fmaf(p[e], a.scale2, -lse2));
+        d[e] = x * (d[e] - delta);
+        if constexpr (PL == 3) {
+          total += x;
+          rest += d[e];
+          p[e] = x;
+        }
+      }
       wave_priority<PL == 1>();
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         const Frag<PA> f = frag_acc<PA>(d, st);
 #pragma unroll
         for (int db = 0; db < L::DB; ++db)
-          mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, 32 * kb * L::RB, st, db), f, acc[db]);
+          if constexpr (PL == 3) {
+            const Frag<3> c = frag_cols<3, DU, PLANE>(cb, 32 * kb * L::RB, st, db);
+            mma<3>(c, f, acc[db]);
+            Mma<uint16_t>::run(c.v[0], frag_acc<1>(p, st).v[0], pk[db]);
+          } else {
+            mma_acc<PL, PA>(frag_cols<PL, DU, PLANE>(cb, 32 * kb * L::RB, st, db), f, acc[db]);
+          }
       }
-      interleave<PP * 2 * L::DB, PL * 4 * L::DB, 6>();
+      interleave<(PL == 3 ? 7 : PP) * 2 * L::DB, PL * 4 * L::DB, 6>();
       wave_priority<0>();
     }
   }
+  if constexpr (PL == 3) {
+    total = sum32(total);
+    rest = sum32(rest);
+  }
   if constexpr (WS > 1) {
+    float2* const sums = reinterpret_cast<float2*>(smem + JOIN) + wave * 64 + lane;
+    if constexpr (PL == 3) {
+      join_waves<WS, L::DB>(pk, smem, wave, lane);
+      *sums = make_float2(total, rest);
+    }
     if (!join_waves<WS, L::DB>(acc, smem, wave, lane)) return;
+    if constexpr (PL == 3) {
+#pragma unroll
+      for (int w = 1; w < WS; ++w) {
+        total += sums[w * 64].x;
+        rest += sums[w * 64].y;
+      }
+    }
+  }
+  float f = a.scale;
+  if constexpr (PL == 3) {
+    const float norm = row_norm(total, lse2);
+    if (norm != 0.f) {
+      // rows of dS sum to 0; what delta leaves, out being rounded, goes into it
+      f *= norm;
+      rest *= norm;
+#pragma unroll
+      for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = fmaf(-rest, pk[db][e], acc[db][e]);
+    }
+    if (half == 0 && r < s.nq) {
+      a.norm[row] = norm != 0.f ? norm : 1.f;
+      if (norm != 0.f) a.delta[row] = delta + rest;
+    }
   }
   if (r >= s.nq) {
 #pragma unroll
     for (int db = 0; db < L::DB; ++db) acc[db] = zero16();
   }
-  store_row<T, L::DB>(acc, a.scale, at_row_w(a.dq, it.b, s.q0 + iq, head), nullptr, a.dim, half, r < s.q_rows);
+  store_row<T, L::DB>(acc, f, at_row_w(a.dq, it.b, s.q0 + iq, head), nullptr, a.dim, half, r < s.q_rows);
 }
 
-// dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in
-// LDS), the workgroup passes over the queries of one head, or of several heads
+// dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in LDS;
+// of three planes the smallest, where the registers do not hold all), the workgroup passes over the queries of one head, or of several heads
 // of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
 template <int PL, int DU, int BM, int WS, int NST, bool VL, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
@@ -1043,11 +1110,11 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
   using L = Lay<DU>;
   using T = typename Io<PL>::T;
   constexpr int BK = 128 / WS, SR = BM * WS, PLANE = SR * L::RB, TILE = PL * PLANE, STAGE = 2 * TILE;
-  constexpr int VPLANE = BK * L::RB, VT = VL ? PL * VPLANE : 0;
+  constexpr int VPLANE = BK * L::RB, VT = VL ? VPLANE : 0;
   constexpr int JOIN = (WS - 1) * (4 / WS) * L::DB * 4096;
   static_assert(SR <= 128, "the rows' statistics");
   // V, the stages of Q and dO, those of the rows' statistics (128 floats of each kind)
-  constexpr int USED = VT + NST * (STAGE + 1024);
+  constexpr int STATS = PL == 3 ? 1536 : 1024, USED = VT + NST * (STAGE + STATS);
   __shared__ __attribute__((aligned(1024))) char smem[USED > JOIN ? USED : JOIN];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1096,16 +1163,30 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
     if (wave < 2 || SR > 64) {
       const float* p = (wave & 1 ? a.delta : a.lse2) + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q;
       load_lds4(reinterpret_cast<const char*>(p), min(min((wave >> 1) * 64 + lane, SR - 1), left - 1) * 4,
-                stats + i % NST * 1024 + (wave & 1) * 512 + (wave >> 1) * 256);
+                stats + i % NST * STATS + (wave & 1) * 512 + (wave >> 1) * 256);
+    }
+    if (PL == 3 && (SR > 64 ? wave < 2 : wave == 2)) {
+      const int at64 = SR > 64 ? wave * 64 : 0;
+      load_lds4(reinterpret_cast<const char*>(a.norm + srow + nh * static_cast<int64_t>(a.seqs.q_tokens) + q),
+                min(min(at64 + lane, SR - 1), left - 1) * 4, stats + i % NST * STATS + 1024 + at64 * 4);
     }
     if (++nt == t0 + per) { nt = t0; ++nh; }
   };
   if (NST > 1 && steps > 0) issue(0);
 
-  Frag<PL> kf[L::STEPS], vf[VL ? 1 : L::STEPS];
+  constexpr int VR = PL - VL;  // V's planes in registers
+  Frag<PL> kf[L::STEPS];
+  Frag<VR ? VR : 1> vf[VR ? L::STEPS : 1];
   const int r = w0 + (lane & 31), j = min(r, s.k_rows - 1);
   load_operand<PL, DU>(at_row(a.k, it.b, s.k0 + j, it.kvh), a.dim, half, kf);
-  if constexpr (!VL) load_operand<PL, DU>(at_row(a.v, it.b, s.k0 + j, it.kvh), a.dim, half, vf);
+  if constexpr (VR > 0) {
+#pragma unroll
+    for (int st = 0; st < L::STEPS; ++st) {
+      const Frag<PL> f = load_chunk<PL>(at_row(a.v, it.b, s.k0 + j, it.kvh), 2 * st + half, a.dim);
+#pragma unroll
+      for (int p = 0; p < VR; ++p) vf[st].v[p] = f.v[p];
+    }
+  }
   const int qmin = a.causal ? j - shift : 0;
   const int qmax = a.causal && a.window ? min(s.nq - 1, j - shift + a.window - 1) : s.nq - 1;
   if constexpr (VL) {
@@ -1113,8 +1194,7 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
       for (int p = threadIdx.x; p < BK * L::CH; p += 256) {
         const int vr = p / L::CH, c = p % L::CH;
         const Frag<PL> f = load_chunk<PL>(at_row(a.v, it.b, s.k0 + min(k0 + vr, s.nk - 1), it.kvh), c, a.dim);
-#pragma unroll
-        for (int q = 0; q < PL; ++q) *reinterpret_cast<u32x4_t*>(smem + q * VPLANE + L::at(vr, c)) = f.v[q];
+        *reinterpret_cast<u32x4_t*>(smem + L::at(vr, c)) = f.v[PL - 1];
       }
   }
   f32x16_t dk[L::DB], dv[L::DB];
@@ -1131,7 +1211,7 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
     __syncthreads();
     if (NST > 1 && i + 1 < steps) issue(i + 1);
     const uint32_t rb = rbase + i % NST * STAGE, cb = cbase + i % NST * STAGE;
-    const uint32_t sb = stats + i % NST * 1024 + ws * BM * 4 + 16 * half;
+    const uint32_t sb = stats + i % NST * STATS + ws * BM * 4 + 16 * half;
     const int q0 = ct * SR + ws * BM;
     if (++ct == t0 + per) ct = t0;
 #pragma unroll
@@ -1147,10 +1227,13 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
         const Frag<PL> f = frag_rows<PL, PLANE>(rb, TILE + 32 * qk * L::RB, st);
-        if constexpr (VL) mma<PL, true>(f, frag_rows<PL, VPLANE>(vbase, 0, st), d);
-        else mma<PL, true>(f, vf[st], d);
+        Frag<PL> v;
+        if constexpr (VL) v.v[PL - 1] = frag_rows<1, VPLANE>(vbase, 0, st).v[0];
+#pragma unroll
+        for (int p = 0; p < VR; ++p) v.v[p] = vf[st].v[p];
+        mma<PL, true>(f, v, d);
       }
-      interleave<PR * 2 * L::STEPS, PL * (VL ? 3 : 2) * L::STEPS, 6>();
+      interleave<PR * 2 * L::STEPS, (2 * PL + VL) * L::STEPS, 6>();
       wave_priority<0>();
       if (q + 32 > s.nq || (a.causal && q + shift < w0 + 31) ||
           (a.causal && a.window && q + 31 + shift - w0 >= a.window)) {
@@ -1165,9 +1248,12 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const u32x4_t ls = lds16(sb + (32 * qk + 8 * g) * 4), de = lds16(sb + 512 + (32 * qk + 8 * g) * 4);
+        u32x4_t norm;
+        if constexpr (PL == 3) norm = lds16(sb + 1024 + (32 * qk + 8 * g) * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = exp2_(fmaf(p[4 * g + e], a.scale2, -__uint_as_float(ls[e])));
+          float x = exp2_(fmaf(p[4 * g + e], a.scale2, -__uint_as_float(ls[e])));
+          if constexpr (PL == 3) x *= __uint_as_float(norm[e]);
           p[4 * g + e] = x;
           d[4 * g + e] = x * (d[4 * g + e] - __uint_as_float(de[e]));
         }
@@ -1521,7 +1607,8 @@ hipError_t dkv_of(const AttnArgs& a, hipStream_t st) {
 //     121), 384: 59 / 51 / 58 (184 / 149 / 173), 512: 61 / 58 / 75 (192 / 174 /
 //     221), 512 of 1024 tokens: 20 / 23 / 34 (60 / 65 / 96)
 //   windows of 1024, heads of 128, 384: 44 / 66 / 106 (125 / 196 / 296)
-//   fp32, 1024 tokens, WS = 1 / 2 (more than 64 elements) or 4 (one stage in LDS):
+//   fp32, 1024 tokens, WS = 1 / 2 (more than 64 elements) or 4 (one stage in LDS;
+//   gradients before their rows were normalised, which takes 4% more):
 //     128, no mask, 128: 93 / 70 (313 / 196), 192: 95 / 127 (322 / 360); causal,
 //     256: 96 / 84 (329 / 231), 320: 100 / 112 (344 / 323)
 //     64, no mask, 128: 55 / 55 (159 / 140), 192: 57 / 77 (164 / 205); causal,
@@ -1667,7 +1754,7 @@ hipError_t run_attention_backward(AttnArgs a, int dtype, hipStream_t st, LaunchT
       else r = ws_q == 2 ? dq_of<1, DU, 32, 2, 2>(a, st) : dq_of<1, DU, 64, 1, 2>(a, st);
     }
     if (r != hipSuccess || a.seqs.k_tokens == 0) return r;
-    if (dtype != DT_BF16) return ws_k > 1 ? dkv_of<3, DU, 32, WS3, 1, false>(a, st) : dkv_of<3, DU, 32, 1, 2, false>(a, st);
+    if (dtype != DT_BF16) return ws_k > 1 ? dkv_of<3, DU, 32, WS3, 1, false>(a, st) : dkv_of<3, DU, 32, 1, 2, DU == 128>(a, st);
     if (fine_of(a)) return ws_k == 4 ? dkv_of<1, DU, 32, 4, 2, VL, true>(a, st) : dkv_of<1, DU, 32, 1, 2, VL, true>(a, st);
     if (ws_k == 4) return dkv_of<1, DU, 32, 4, 2, VL>(a, st);
     return ws_k == 2 ? dkv_of<1, DU, 32, 2, 2, VL>(a, st) : dkv_of<1, DU, 32, 1, 2, VL>(a, st);

@@ -395,3 +395,44 @@ def test_refusals_leave_buffers_alone(muon):
         muon.attention_backward(do[:, :5], q, k, v, out, torch.zeros(1, 4, 70, device="cuda"))
     torch.cuda.synchronize()
     assert (out == 3).all()
+
+
+@pytest.mark.parametrize("case", [(2, 70, 90, 2, 1, 16, False, 0), (1, 300, 300, 2, 2, 128, True, 0),
+                                  (40, 65, 100, 16, 8, 64, False, 0)], ids=str)
+def test_gradients_do_not_feel_the_rounding_of_lse(muon, case):
+    """fp32: a step of lse (here 2^-18, lse being 40 to 64) would be a common
+    factor 1 + 3.8e-6 of a row's probabilities.  They sum to 1 by themselves up
+    to exp2's own 2^-23 and that of its argument near the maximum, so that
+    gradients agree to a few 2^-23 of their norm.  A sum that lse itself puts
+    elsewhere stays: half a unit more scales by exp(-1/2)."""
+    import torch
+    q, k, v, do = make(case, "f32", 2.0)
+    scale = 3.0 / case[5] ** 0.5
+    kw = dict(causal=case[6], scale=scale)
+    out, lse = muon.attention(q, k, v, **kw)
+    assert lse[:, :, -1].max() > 8
+    ref_ = muon.attention_backward(do, q, k, v, out, lse, **kw)
+    step = 2.0 ** -18
+    near = muon.attention_backward(do, q, k, v, out, lse + step, **kw)
+    far = muon.attention_backward(do, q, k, v, out, lse + 0.5, **kw)
+    for x, y, z in zip(ref_, near, far):
+        x, y, z = (t.double().cpu() for t in (x, y, z))
+        assert (x - y).norm() <= 1e-6 * x.norm()
+        assert (x * np.exp(-0.5) - z).norm() <= 2e-5 * x.norm()
+
+
+@pytest.mark.parametrize("dtype,limit", [("bf16", 3 * 2.0 ** -8), ("f32", 1e-5)])
+def test_gradients_of_a_part_of_the_keys(muon, dtype, limit):
+    """lse and out of all keys: each part's dk and dv are those of the whole
+    call, the parts' dq add up to its own.  bf16: probabilities and two results
+    rounded, 2^-8 each."""
+    import torch
+    q, k, v, do = make((2, 150, 260, 4, 2, 64, False, 0), dtype, 1.5)
+    res = torch.empty_like(q) if dtype == "bf16" else None
+    out, lse = muon.attention(q, k, v, residual=res)
+    whole = muon.attention_backward(do, q, k, v, out, lse, residual=res)
+    cuts = (slice(0, 70), slice(70, 260))
+    parts = [muon.attention_backward(do, q, k[:, c], v[:, c], out, lse, residual=res) for c in cuts]
+    joined = (sum(p[0].double() for p in parts), *(torch.cat([p[i] for p in parts], 1).double() for i in (1, 2)))
+    for x, y in zip(whole, joined):
+        assert (x.double() - y).norm() <= limit * x.double().norm()
