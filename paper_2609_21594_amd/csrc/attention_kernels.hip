@@ -344,7 +344,8 @@ __device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row,
 }
 
 // fp32 arrays that tiles are staged from, as planes: rows [batch][heads]
-// [tokens][3][head, padded to 8].  A thread has 8 elements.
+// [tokens][3][head, padded to 8].  A thread has 8 elements.  (4 us for a small
+// call; without it every workgroup would split the tiles that it shares with others.)
 struct SplitArgs {
   Heads from[4];
   char* to[4];
@@ -569,6 +570,14 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 // and one has its products while the other has its softmax).  WS > 1: WS waves
 // share their queries and take every WS-th tile, and are joined at the end; for
 // requests with too few rows to fill the device.
+//
+// Bound by MFMA and vector issue together: per 64 keys and 32 queries of 128
+// elements 32 MFMAs (1024 cycles) and 32 x 4.2 vector instructions, of which 32
+// are exponentials (about 1000), overlapped across the waves of a SIMD in part
+// (MFMAs busy 55%, vector issue 53% of a busy CU's cycles, LDS 28%, no bank
+// conflicts).  4096 tokens, 32 heads on 8 of 128, causal: 136 us, 1015 TFLOP/s; 2
+// x 8192 without a mask: 1142; 4 x 4096, 16 heads of 64: 932; fp32, 2 x 2048, 16
+// heads of 128: 170.  Few rows: by memory, 268 MB of keys and values in 43 us.
 // ---------------------------------------------------------------------------
 template <int PL, int DU, int BN, int WS, int NST, bool FINE, bool SPLIT, int NW>
 __global__ __launch_bounds__(64 * NW, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
@@ -797,7 +806,7 @@ __global__ __launch_bounds__(64 * NW, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) 
   }
 }
 
-// Joins the splits: a workgroup a row, 32 lanes along the head (4 elements
+// Joins the splits (4 to 5 us for 128 rows of 16 parts): a workgroup a row, 32 lanes along the head (4 elements
 // each) times 8 parts of the splits, summed through LDS in a fixed order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
@@ -931,7 +940,9 @@ __device__ __forceinline__ float row_dots(const Frag<PL>* df, const char* out, c
 // First it forms each row's dout . out in fp32, with what the rounding took
 // from out where the caller kept it, and writes it and log2 of the sum of
 // exponentials for k_attn_dkv: +inf where no key is visible, so that every
-// probability recomputed from it is 0.
+// probability recomputed from it is 0.  Bound as the forward pass is, with half
+// more products: 4096 tokens, 32 heads on 8 of 128, causal: 220 us (206 GFLOP,
+// MFMAs busy 55%).
 template <int PL, int DU, int BN, int WS, int NST, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
   constexpr int PA = kAccPlanes<PL, FINE>;
@@ -1102,7 +1113,10 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
 
 // dK, dV: a wave holds 32 keys (K rows in registers, V rows there or, VL, in LDS;
 // of three planes the smallest, where the registers do not hold all), the workgroup passes over the queries of one head, or of several heads
-// of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+// of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  Its two
+// accumulators and K leave no registers for a second row of queries, so that a
+// step has 32 of them; V's place in LDS frees what two waves a SIMD need.  The
+// case above: 274 us (275 GFLOP, MFMAs busy 55%, LDS 41%).
 template <int PL, int DU, int BM, int WS, int NST, bool VL, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
   constexpr int PA = kAccPlanes<PL, FINE>;
@@ -1296,6 +1310,7 @@ __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(At
 }
 
 // Sums the parts of each group, in order: a thread has 4 elements of dk or dv.
+// At memory's rate: 134 MB in 23 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
   const int quads = a.dim / 4;
@@ -1331,8 +1346,8 @@ __global__ __launch_bounds__(256) void k_attn_sum_heads(AttnArgs a) {
 // ---------------------------------------------------------------------------
 // Rotary positions.  A workgroup takes a few tokens: their angles once (fp64
 // product and reduction to a fraction of a turn, then fp32 sine and cosine),
-// through LDS to every head.  HBM-bound: each element is read and written
-// once.
+// through LDS to every head.  HBM-bound: each element is read and written once
+// (8192 tokens of 40 heads of 128 bf16, 168 MB, in 28 us).
 // ---------------------------------------------------------------------------
 // Unit u of a head: a piece that turns (u < turning), else one that is copied.
 template <typename T>
@@ -1430,7 +1445,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int per_block) {
 
 // ---------------------------------------------------------------------------
 // The clip.  A workgroup has a few rows of one entry; rows whose factor is 1
-// are not touched.  HBM-bound on the rows that change.
+// are not touched.  HBM-bound on the rows that change: 671 MB in 120 us.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float clip_gamma(float m, float threshold) {
   return m > threshold && m < kInf ? fmaxf(threshold / m, 0x1p-126f) : 1.f;  // (0 would have no root to divide by)
@@ -1770,9 +1785,12 @@ hipError_t run_rotary(const RotaryArgs& a, int dtype, hipStream_t st, LaunchTime
   const int64_t all = a.batch * a.tokens;
   if (all == 0) return hipSuccess;
   Timed tm(timer, KK_ROTARY, st);
-  // a few tokens a workgroup, fewer where that leaves compute units idle
-  int per = std::max(1, std::min(8, kRotPairs / std::max(1, a.rot / 2)));
-  while (per > 1 && (all + per - 1) / per < 1024) per /= 2;
+  // tokens a workgroup, 1 / 2 / 4 / 8, us on an MI355X: 2048 of 16 heads of 64 fp32
+  // 5.7 / 5.1 / 5.2 / 6.3; 4094 of 24 of 96 fp32 15.6 / 15.4 / 15.5 / 20.3; 8192 of
+  // 40 of 128 bf16 27.4 / 27.9 / 28.1 / 28.4, 1024: 6.1 / 6.1 / 7.1 / 10.5, 256: 4.3 /
+  // 4.9 / 6.2 / 9.6
+  int per = std::max(1, std::min(2, kRotPairs / std::max(1, a.rot / 2)));
+  if ((all + per - 1) / per < 512) per = 1;
   const dim3 g(static_cast<unsigned>((all + per - 1) / per)), b(256);
   if (dtype == DT_BF16) hipLaunchKernelGGL((k_rotary<uint16_t>), g, b, 0, st, a, per);
   else hipLaunchKernelGGL((k_rotary<float>), g, b, 0, st, a, per);
