@@ -83,7 +83,8 @@ class MuonHeads(ctypes.Structure):
 class MuonAttention(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("fill_rest", ctypes.c_int32), ("reserved", ctypes.c_int32), ("batch", ctypes.c_int64), ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
+                ("fill_rest", ctypes.c_int32), ("reserved", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64),
                 ("sequences", ctypes.c_int64), ("window", ctypes.c_int64),
                 ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p),
                 ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p),
@@ -393,6 +394,12 @@ def _heads(t):
     return (t.data_ptr(), st[0], st[1], st[2]) if len(st) == 4 else (t.data_ptr(), 0, st[0], st[1])
 
 
+def _empty(t):
+    """A new contiguous tensor like t (its shape given anew takes longer)."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 class _Attention:
     """One attention request: checks that need the tensors' shapes, then the
     library's packed record."""
@@ -426,15 +433,14 @@ class _Attention:
         sq, hq, d = q.shape[-3:]
         sk, hkv = k.shape[-3], k.shape[-2]
         self.lse_shape = (hq, sq) if packed else (batch, hq, sq)
-        self.q_shape, self.k_shape = q.shape, k.shape
         self.start = (self.code, d, hq, hkv, int(bool(causal)), float(d) ** -0.5 if scale is None else float(scale))
         self.head = (0, batch, sq, sk, seqs, int(window),
                      *(0 if t is None else t.data_ptr() for t in self.lists), *_heads(q), *_heads(k), *_heads(v))
 
     def record(self, out, residual, lse, max_logits, scratch, scratch_bytes, fill=0):
-        return _ATTENTION_PACK.pack(*self.start, fill, *self.head, *_heads(out), *(_NO_HEADS if residual is None else _heads(residual)),
-                                    lse.data_ptr(), 0 if max_logits is None else max_logits.data_ptr(), scratch,
-                                    scratch_bytes)
+        return _ATTENTION_PACK.pack(*self.start, fill, *self.head, *_heads(out),
+                                    *(_NO_HEADS if residual is None else _heads(residual)), lse.data_ptr(),
+                                    0 if max_logits is None else max_logits.data_ptr(), scratch, scratch_bytes)
 
     def sizes(self):
         """The record with no outputs yet, for muon_attention_scratch."""
@@ -634,8 +640,8 @@ class Muon:
     # ---- the attention block of a training step ---------------------------------
 
     def _stream(self):
-        import torch
-        return torch.cuda.current_stream(self.device).cuda_stream
+        import torch  # (torch.cuda.current_stream makes an object: a tenth of a small call)
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def _scratch(self, record, backward, like):
         """(keepalive, pointer, bytes) of the scratch memory a request needs,
@@ -683,7 +689,7 @@ class Muon:
         keep, at, n = self._scratch(a.sizes(), 0, q)
         # rows of no packed sequence: zeros in a new tensor, left alone in a given one
         fill = int(q_offsets is not None and out is None)
-        out = q.new_empty(a.q_shape) if out is None else out
+        out = _empty(q) if out is None else out
         lse = q.new_empty(a.lse_shape, dtype=torch.float32)
         if q_offsets is not None and not fill:
             lse.fill_(-float("inf"))
@@ -716,10 +722,10 @@ class Muon:
             raise ValueError("lse must be contiguous")
         keep, at, n = self._scratch(a.sizes(), 1, q)
         fill = int(q_offsets is not None and dq is None and dk is None and dv is None)
-        new = q.new_zeros if q_offsets is not None and not fill else q.new_empty
-        dq = new(a.q_shape) if dq is None else dq
-        dk = new(a.k_shape) if dk is None else dk
-        dv = new(a.k_shape) if dv is None else dv
+        new = (lambda t: t.new_zeros(t.shape)) if q_offsets is not None and not fill else _empty
+        dq = new(q) if dq is None else dq
+        dk = new(k) if dk is None else dk
+        dv = new(v) if dv is None else dv
         grad = _GRAD_PACK.pack(*_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv))
         self._check(self.lib.muon_attention_backward(self.h, a.record(out, residual, lse, None, at, n, fill), grad,
                                                      self._stream()))
@@ -770,7 +776,7 @@ class Muon:
                 _expect(y, t.shape, t.dtype, "out")
         _check_device([*xs, freqs, *([] if positions is None else [positions]), *(outs or [])], self.device)
         if outs is None:
-            outs = [t.new_empty(t.shape) for t in xs]
+            outs = [_empty(t) for t in xs]
         batch, tokens = lead if len(lead) == 2 else (1, lead[0])
         pst = (0, 0) if positions is None else (positions.stride() if len(lead) == 2 else (0, positions.stride(0)))
         rec = _ROTARY_PACK.pack(_dtype_code(x), d, 2 * freqs.numel(), int(layout == "interleaved"),
