@@ -826,7 +826,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s = part; s < a.splits; s += 8) {
     const float2 v = a.part_ml[s * all + row];
-    if (v.x == -kInf) continue;  // a part that sees nothing
+    if (v.x == -kInf && v.y == 0.f) continue;  // a part that sees nothing (one of NaN alone has no maximum either)
     const float w = exp2_(v.x - m);
     l = fmaf(w, v.y, l);
     if (d < a.dim) {
