@@ -19,12 +19,15 @@ process with it.  Both are refused with a RuntimeError where these functions
 can see them: a captured backward pass of an eager forward pass, and leaves
 given to them that an earlier call of theirs on another stream still holds.
 (`Muon.attention` and `Muon.attention_backward` know no autograd.)
+
+Forward-mode tangents are refused with a RuntimeError, with gradients enabled or not.
 """
 from __future__ import annotations
 
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 
 def rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, method="none", original_length=None, low=1.0, high=32.0):
@@ -62,6 +65,14 @@ def rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, method="none", orig
     elif method != "base":
         raise ValueError(f"unknown method {method!r}")
     return freqs
+
+
+def _refuse_tangents(*tensors):
+    """There are no forward-mode derivatives here, and `no_grad` leaves that mode on:
+    without this a result would come back without its tangent."""
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise RuntimeError("rotary and attention have no forward-mode derivative (jvp)")
 
 
 def _enter(ctx, tensors):
@@ -120,6 +131,7 @@ def rotary(lib, xs, freqs, positions=None, first=0, layout="half", scale=1.0, in
     """`Muon.rotary` with gradients: a tensor, or a list of up to 4."""
     one = torch.is_tensor(xs)
     xs = [xs] if one else list(xs)
+    _refuse_tangents(*xs, freqs)
     kw = dict(first=first, layout=layout, scale=scale, inverse=inverse)
     if torch.is_grad_enabled():
         ys = _Rotary.apply(lib, freqs, positions, kw, *xs)
@@ -161,6 +173,7 @@ def attention(lib, q, k, v, scale=None, causal=False, window=0, q_offsets=None, 
               k_lens=None, max_logits=None, return_lse=False):
     """`Muon.attention` with gradients for q, k and v (lse and max_logits carry
     none).  bf16 outputs keep what their rounding took for the backward pass."""
+    _refuse_tangents(q, k, v)
     kw = dict(scale=scale, causal=causal, window=window, q_offsets=q_offsets, k_offsets=k_offsets, q_lens=q_lens,
               k_lens=k_lens)
     if torch.is_grad_enabled():

@@ -1,0 +1,68 @@
+"""The attention block's autograd functions and host-only checks on the CPU, with a
+stand-in for the library where tensors would need a device."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import torch.autograd.forward_ad as fwd  # noqa: E402
+
+from paper_2609_21594_amd.attention import attention, rotary  # noqa: E402
+
+
+class StandIn:
+    """Results of the right shapes; says whether it was called."""
+    calls = 0
+
+    def attention(self, q, k, v, max_logits=None, residual=None, **kw):
+        self.calls += 1
+        return q.detach().clone(), torch.zeros(q.shape[0], q.shape[2], q.shape[1])
+
+    def rotary(self, xs, freqs, positions=None, **kw):
+        self.calls += 1
+        return [x.detach().clone() for x in xs]
+
+
+# ---------------------------------------------------------------- forward-mode tangents
+
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("which", range(3))
+def test_attention_refuses_tangents(grad, which):
+    """There is no forward-mode derivative; no_grad does not turn that mode off, so a
+    result without a tangent would be a wrong derivative of zero."""
+    xs = [torch.ones(1, 3, 2, 8) for _ in range(3)]
+    with fwd.dual_level(), torch.set_grad_enabled(grad):
+        xs[which] = fwd.make_dual(xs[which], torch.ones(1, 3, 2, 8))
+        lib = StandIn()
+        with pytest.raises(RuntimeError, match="jvp"):
+            attention(lib, *xs)
+        assert lib.calls == 0
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_rotary_refuses_tangents(grad):
+    x, freqs = torch.ones(1, 3, 2, 8), torch.ones(4, dtype=torch.float64)
+    with fwd.dual_level(), torch.set_grad_enabled(grad):
+        dual = fwd.make_dual(x, torch.ones_like(x))
+        with pytest.raises(RuntimeError, match="jvp"):
+            rotary(StandIn(), dual, freqs)
+        with pytest.raises(RuntimeError, match="jvp"):
+            rotary(StandIn(), [x, dual], freqs)
+        with pytest.raises(RuntimeError, match="jvp"):
+            rotary(StandIn(), x, fwd.make_dual(freqs, torch.ones_like(freqs)))
+
+
+def test_transformed_functions_refuse_tangents():
+    def f(x):
+        with torch.no_grad():
+            return attention(StandIn(), x, x, x)
+    x = torch.ones(1, 3, 2, 8)
+    with pytest.raises(RuntimeError, match="jvp"):
+        torch.func.jvp(f, (x,), (x,))
+
+
+def test_without_tangents_no_grad_skips_autograd():
+    lib, x = StandIn(), torch.ones(1, 3, 2, 8, requires_grad=True)
+    with fwd.dual_level(), torch.no_grad():
+        assert not attention(lib, x, x, x).requires_grad
+        assert not rotary(lib, x, torch.ones(4, dtype=torch.float64)).requires_grad
+    assert lib.calls == 2
