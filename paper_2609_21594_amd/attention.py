@@ -128,12 +128,15 @@ def _plain(g):
 
 
 def rotary(lib, xs, freqs, positions=None, first=0, layout="half", scale=1.0, inverse=False):
-    """`Muon.rotary` with gradients: a tensor, or a list of up to 4."""
+    """`Muon.rotary` with gradients: a tensor, or a list of up to 4.  freqs have
+    none, and are refused where they ask for one."""
     one = torch.is_tensor(xs)
     xs = [xs] if one else list(xs)
     _refuse_tangents(*xs, freqs)
     kw = dict(first=first, layout=layout, scale=scale, inverse=inverse)
     if torch.is_grad_enabled():
+        if freqs.requires_grad:
+            raise RuntimeError("rotary has no gradient for freqs: detach them")
         ys = _Rotary.apply(lib, freqs, positions, kw, *xs)
     else:
         ys = lib.rotary(xs, freqs, positions=positions, **kw)

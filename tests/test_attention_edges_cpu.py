@@ -66,3 +66,16 @@ def test_without_tangents_no_grad_skips_autograd():
         assert not attention(lib, x, x, x).requires_grad
         assert not rotary(lib, x, torch.ones(4, dtype=torch.float64)).requires_grad
     assert lib.calls == 2
+
+
+# ---------------------------------------------------------------- gradients that do not exist
+
+def test_rotary_refuses_frequencies_that_want_a_gradient():
+    """It has none for them; silence would leave them untrained."""
+    lib, x = StandIn(), torch.ones(1, 3, 2, 8)
+    freqs = torch.ones(4, dtype=torch.float64, requires_grad=True)
+    with pytest.raises(RuntimeError, match="freqs"):
+        rotary(lib, x, freqs)
+    with torch.no_grad():
+        rotary(lib, x, freqs)
+    assert lib.calls == 1
