@@ -343,7 +343,7 @@ typedef struct {
   int32_t head_dim;        /* multiple of 8 (bf16) or 4 (fp32), 128 at most */
   int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
   int32_t causal;          /* 0 or 1 */
-  float scale;             /* finite, > 0 */
+  float scale;             /* > 0, and scale * log2(e) finite (2.35e38 at most) */
   int32_t fill_rest;       /* packed: 1 writes zeros (lse: -inf) to the rows of
                               outputs that no sequence holds; 0 leaves them */
   int32_t reserved;        /* must be 0 */

@@ -108,6 +108,9 @@ Extent extent(const void* p, int64_t bytes) {
   return Extent{lo, lo + uintptr_t(bytes)};
 }
 
+// What the kernels multiply logits with, for exponentials of base 2.
+float scale2_of(const muon_attention_t* a) { return float(double(a->scale) * 1.4426950408889634074); }
+
 // Sizes alone.
 muon_status_t check_sizes(const muon_attention_t* a, Why& why) {
   if (!a) return why.invalid("the request is NULL");
@@ -125,7 +128,8 @@ muon_status_t check_sizes(const muon_attention_t* a, Why& why) {
   if ((a->fill_rest != 0 && a->fill_rest != 1) || (a->fill_rest && !a->q_offsets))
     return why.invalid("fill_rest must be 0 or 1, and needs offsets");
   if (a->reserved != 0) return why.invalid("reserved must be 0");
-  if (!std::isfinite(a->scale) || !(a->scale > 0.f)) return why.invalid("scale must be finite and > 0");
+  if (!std::isfinite(a->scale) || !(a->scale > 0.f) || !std::isfinite(scale2_of(a)))
+    return why.invalid("scale must be > 0, and scale * log2(e) finite");
   if (a->window < 0 || (a->window > 0 && !a->causal)) return why.invalid("window must be >= 0, and needs causal");
   if (!a->q_offsets != !a->k_offsets) return why.invalid("q_offsets and k_offsets go together");
   if (!a->q_lengths != !a->k_lengths) return why.invalid("q_lengths and k_lengths go together");
@@ -269,7 +273,7 @@ muon_status_t check_attention(const muon_attention_t* a, const muon_attention_gr
   k.window = window_of(a);
   k.fill = a->fill_rest;
   k.scale = a->scale;
-  k.scale2 = float(double(a->scale) * 1.4426950408889634074);
+  k.scale2 = scale2_of(a);
   k.splits = p.splits;
   k.kv_parts = p.kv_parts;
   char* const s = static_cast<char*>(a->scratch);

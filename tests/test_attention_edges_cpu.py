@@ -79,3 +79,15 @@ def test_rotary_refuses_frequencies_that_want_a_gradient():
     with torch.no_grad():
         rotary(lib, x, freqs)
     assert lib.calls == 1
+
+
+# ---------------------------------------------------------------- requests
+
+def test_scales_that_binary32_cannot_hold_in_base_2_are_refused():
+    """The kernels take scale * log2(e), which must be finite: with infinity a logit
+    of 0 becomes NaN."""
+    from tests.test_attention_cpu import check, grads, request
+    assert check(request(scale=2.3e38))[0] == 0
+    for g in (None, grads()):
+        st, msg = check(request(scale=3e38), g)
+        assert st == 1 and "scale" in msg
