@@ -50,3 +50,26 @@ def test_keys_that_are_no_numbers_reach_every_row_that_sees_them(muon, dtype):  
             bad[:, lo:lo + n, :, 7] = NAN
             out, lse = muon.attention(q, bad, v, causal=True)
             assert torch.isnan(out).all() and torch.isnan(lse).all(), (n, lo)
+
+
+@pytest.mark.parametrize("heads,d", [(16, 8), (8, 72), (1, 8), (1, 72)], ids=str)
+def test_rows_of_equal_probabilities_sum_to_one(muon, heads, d):  # noqa: F811
+    """fp32, logits all 0: one query on n keys has p = 1 / n, and dv of a gradient of
+    ones is p.  The gradient pass normalises rows by their own sums, so that what is
+    left of a common factor is those sums' rounding, in half steps of 2^-24: 4 for 16
+    values by pairs, 2 for the steps with their carries, 1 for the halves of a wave, 3
+    for up to four waves a row; 1 each for the reciprocal, its product with p, and
+    dv's product and its sum with zeros."""
+    import torch
+    b, s = 64, 1600
+    nk = torch.linspace(200, 1598, b).to(torch.int32).cuda()   # odd and even, whole tiles and not
+    one = torch.ones_like(nk)
+    rng = np.random.default_rng(4)
+    q = torch.zeros(b, 1, heads, d, device="cuda")
+    k, v = (torch.from_numpy(rng.standard_normal((b, s, heads, d)).astype(np.float32)).cuda() for _ in "kv")
+    out, lse = muon.attention(q, k, v, q_lens=one, k_lens=nk)
+    _, _, dv = muon.attention_backward(torch.ones_like(q), q, k, v, out, lse, q_lens=one, k_lens=nk)
+    for i, n in enumerate(nk.tolist()):
+        off = (dv[i, :n].double() * n - 1).abs().max()
+        assert off <= 14 * 2.0 ** -24, (n, float(off))
+        assert not dv[i, n:].any()
