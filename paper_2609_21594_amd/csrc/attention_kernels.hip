@@ -217,6 +217,15 @@ struct Stager {
   }
 };
 
+// 4 elements, aligned to their size.
+template <typename T>
+__device__ __forceinline__ float4 load4(const char* p) {
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(p);
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xffff0000u));
+}
+
 // 8 elements from c * 8 on of a row (zeros from `dim` on), as operand planes.
 template <int PL>
 __device__ __forceinline__ Frag<PL> load_chunk(const char* row, int c, int dim) {
@@ -304,11 +313,13 @@ __device__ __forceinline__ f32x16_t zero16() {
 }
 
 // Writes the lane's row (a transposed accumulator: element 32 db + 8 g +
-// 4 half + i in register 4 g + i of block db), times `f`.  RES: to `res` goes
-// what the rounding took.  All lanes of the wave call it; `on`: this lane
-// writes.
+// 4 half + i in register 4 g + i of block db), times `f`.  To `res` goes what the
+// rounding took, or nothing where the result is `exact`.  All lanes of the wave
+// call it; `on`: this lane writes.
 template <typename T, int DB>
-__device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row, char* res, int dim, int half, bool on) {
+__device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row, char* res, int dim, int half, bool on,
+                                          bool exact = false) {
+  const uint32_t keep = exact ? 0u : ~0u;
   const int dch = dim / (16 / static_cast<int>(sizeof(T)));
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -320,7 +331,7 @@ __device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row,
         for (int k = 0; k < 4; ++k) {  // k / 2: group 2 p + k / 2, pairs of elements
           const float x = o[db][8 * p + 2 * k] * f, y = o[db][8 * p + 2 * k + 1] * f;
           w[k] = pack_bf16x2(x, y);
-          e[k] = res ? pack_bf16x2(x - __uint_as_float(w[k] << 16), y - __uint_as_float(w[k] & 0xffff0000u)) : 0u;
+          e[k] = res ? pack_bf16x2(x - __uint_as_float(w[k] << 16), y - __uint_as_float(w[k] & 0xffff0000u)) & keep : 0u;
         }
         // halves exchange so that each lane holds 8 consecutive elements
         const uint2 a = swap32(w[0], w[2]), b = swap32(w[1], w[3]);
@@ -341,6 +352,24 @@ __device__ __forceinline__ void store_row(const f32x16_t* o, float f, char* row,
       }
     }
   }
+}
+
+// A row that sees one key has that key's value, exactly.  p / sum p is 1 but for
+// the exponent's rounding, which the sum holds to 24 bits and an operand of p may
+// not.  bf16: what the quotient rounds to is the value, and the rounding took
+// nothing.  fp32: a tenth of such rows would be a step off, and its gradients not
+// 0, so they take the value itself: here as an accumulator's row, where `on`.
+template <int DB>
+__device__ __forceinline__ void take_row(f32x16_t* o, const char* row, int dim, int half, bool on) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * db + 8 * g + 4 * half;
+      if (!on || d >= dim) continue;
+      const float4 x = *reinterpret_cast<const float4*>(row + d * 4);
+      o[db][4 * g] = x.x; o[db][4 * g + 1] = x.y; o[db][4 * g + 2] = x.z; o[db][4 * g + 3] = x.w;
+    }
 }
 
 // fp32 arrays that tiles are staged from, as planes: rows [batch][heads]
@@ -786,14 +815,21 @@ __global__ __launch_bounds__(64 * NW, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) 
     return;
   }
   const bool live = in && iq < s.nq;
-  const float inv = !live || l == 0.f ? 0.f : 1.f / l;
+  const bool one = live && jmin == jmax && l > 0.f && l < kInf;  // (NaN stays)
+  float inv = !live || l == 0.f ? 0.f : 1.f / l;
+  if constexpr (PL == 3) {
+    if (__any(one)) take_row<L::DB>(o, at_row(a.v, it.b, s.k0 + jmin, it.kvh), a.dim, half, one);
+    if (one) inv = 1.f;
+  } else if (PA == 1 && one) {
+    inv = 1.f / to_f32<uint16_t>(f32_to_bf16(l));  // l is the row's p, and o has its one plane
+  }
   if (!live) {
 #pragma unroll
     for (int db = 0; db < L::DB; ++db) o[db] = zero16();
   }
   char* orow = at_row_w(a.out, it.b, s.q0 + iq, head);
   char* rrow = a.res.p ? at_row_w(a.res, it.b, s.q0 + iq, head) : nullptr;
-  store_row<T, L::DB>(o, inv, orow, rrow, a.dim, half, in);
+  store_row<T, L::DB>(o, inv, orow, rrow, a.dim, half, in, one);
   if (in && half == 0) a.lse[row] = live && l != 0.f ? (m + __log2f(l)) * kLn2 : -kInf;
   if (a.max_logits) {
     float x = live ? top * a.scale : -kInf;
@@ -859,6 +895,13 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const float inv = some ? 1.f / l : 0.f;
   float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
   if (!some) o[0] = o[1] = o[2] = o[3] = 0.f;
+  // the keys that the row sees: 0 .. last, as split passes have no window
+  const int nq = a.seqs.q_len ? clampi(a.seqs.q_len[b], 0, a.seqs.q_tokens) : a.seqs.q_tokens;
+  const int nk = a.seqs.k_len ? clampi(a.seqs.k_len[b], 0, a.seqs.k_tokens) : a.seqs.k_tokens;
+  if (some && l > 0.f && l < kInf && (a.causal ? i + nk - nq : nk - 1) == 0) {  // one: its value (take_row)
+    const float4 y = load4<T>(at_row(a.v, b, 0, head / a.group) + d * sizeof(T));
+    o[0] = y.x; o[1] = y.y; o[2] = y.z; o[3] = y.w;
+  }
   char* orow = at_row_w(a.out, b, i, head);
   if constexpr (sizeof(T) == 2) {
     const uint2 w = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import attention_ref as ref
-from tests.gpu_util import to_host
+from tests.gpu_util import to_bits, to_host
 from tests.test_attention_gpu import close, make, muon  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +73,66 @@ def test_rows_of_equal_probabilities_sum_to_one(muon, heads, d):  # noqa: F811
         off = (dv[i, :n].double() * n - 1).abs().max()
         assert off <= 14 * 2.0 ** -24, (n, float(off))
         assert not dv[i, n:].any()
+
+
+def seen_keys(nq, nk, causal, window):
+    """(first, last) key of each query."""
+    i = np.arange(nq)
+    last = np.minimum(nk - 1, i + nk - nq) if causal else np.full(nq, nk - 1)
+    return np.maximum(0, i + nk - nq - window + 1) if causal and window else np.zeros(nq, dtype=int), last
+
+
+# batch, queries, keys, query heads, key heads, head size, causal, window, lengths of queries and keys
+ONE_KEY = [
+    (3, 1, 1, 4, 2, 72, True, 0, None),
+    (1, 300, 300, 2, 1, 128, True, 1, None),
+    (2, 40, 40, 3, 3, 16, True, 1, None),
+    (2, 200, 1, 4, 4, 64, False, 0, None),
+    (4, 130, 130, 4, 2, 96, True, 0, None),                                  # the first query alone
+    (2, 70, 33, 2, 2, 32, True, 0, None),
+    (40, 150, 150, 4, 4, 64, True, 1, None),                                 # one plane
+    (3, 1, 1500, 4, 1, 128, True, 0, ([1, 1, 0], [1, 1500, 1])),             # parts, heads of a group in a tile
+    (2, 5, 900, 4, 4, 80, False, 0, ([5, 3], [1, 900])),
+    (2, 200, 4100, 4, 2, 64, True, 0, ([200, 150], [100, 1])),               # parts of many queries
+    (8, 2050, 130, 8, 8, 128, True, 1, ([2050, 1, 0, 5, 600, 7, 8, 9], [130, 1, 4, 0, 130, 7, 8, 9])),  # 8 waves
+    (0, 260, 200, 4, 2, 64, True, 0, ([1, 130, 0, 129], [1, 130, 3, 66])),   # packed
+    (0, 70, 70, 2, 2, 40, False, 0, ([1] * 70, [1] * 70)),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", ONE_KEY, ids=str)
+def test_rows_that_see_one_key_have_its_value_and_no_gradient(muon, case, dtype):  # noqa: F811
+    """From the library's own results, logits well above 1: out is the value row bit
+    for bit, and every dS of the row is exactly 0."""
+    import torch
+    b, sq, sk, hq, hkv, d, causal, window, lens = case
+    q, k, v, do = make((max(1, b), sq, sk, hq, hkv, d, causal, window), dtype, 3.0)
+    kw = dict(causal=causal, window=window)
+    if b:
+        nq, nk = lens or ([sq] * b, [sk] * b)
+        seqs = [(n, 0, x, 0, y) for n, (x, y) in enumerate(zip(nq, nk))]
+        if lens:
+            kw.update((n, torch.tensor(x, dtype=torch.int32, device="cuda")) for n, x in (("q_lens", nq), ("k_lens", nk)))
+    else:
+        qo, ko = (np.cumsum([0] + list(x)) for x in lens)
+        seqs = [(0, int(i), x, int(j), y) for i, x, j, y in zip(qo, lens[0], ko, lens[1])]
+        q, k, v, do = (t[0] for t in (q, k, v, do))
+        kw.update((n, torch.from_numpy(x.astype(np.int32)).cuda()) for n, x in (("q_offsets", qo), ("k_offsets", ko)))
+    res = torch.full_like(q, NAN) if dtype == "bf16" else None
+    out, lse = muon.attention(q, k, v, residual=res, **kw)
+    dq, dk, dv = muon.attention_backward(do, q, k, v, out, lse, residual=res, **kw)
+    row = (lambda t, n: t[n]) if b else (lambda t, n: t)
+    value = v.repeat_interleave(hq // hkv, -2)
+    rows = 0
+    for n, i, x, j, y in seqs:
+        first, last = seen_keys(x, y, causal, window)
+        at = np.flatnonzero(first == last)
+        rows += len(at)
+        mine, theirs = torch.from_numpy(i + at).cuda(), torch.from_numpy(j + first[at]).cuda()
+        assert np.array_equal(to_bits(row(out, n)[mine]), to_bits(row(value, n)[theirs])), n
+        assert not row(dq, n)[mine].any(), n
+        assert res is None or not row(res, n)[mine].any(), n
+        lone = np.setdiff1d(first[at], [c for f, l in zip(first, last) if l > f for c in range(f, l + 1)])
+        assert not row(dk, n)[torch.from_numpy(j + lone).cuda()].any(), n
+    assert rows and dv.any()
