@@ -473,8 +473,9 @@ muon_status_t muon_plan_step(const muon_param_t* params, int64_t n, const muon_h
  * apply_x0, adamw, ns_small (the whole step of a chunk whose short side is
  * at most 128, one launch in the count although column slices are 2 K + 2
  * kernels), rotary, attention_forward, attention_backward, qk_clip (each call
- * one launch in the count; the flops of attention are those of its products
- * over the visible pairs of dense sequences).  exec_flops of fp32 Newton-Schulz on the tile kernel counts its
+ * one launch in the count; the flops of attention are 2 products' forward and
+ * 5 products' backward over the visible pairs of the dense request: with lengths
+ * or offsets, which lie on the device, an upper bound).  exec_flops of fp32 Newton-Schulz on the tile kernel counts its
  * six bf16 products.  `reset` != 0 clears the counters after reading. */
 typedef struct {
   const char* name;

@@ -1592,9 +1592,15 @@ int64_t tiles_of(const Seqs& s, int64_t tokens, int bt) {
 }
 // The tiles of a launch: one more for the rows that no sequence holds.
 int64_t launch_tiles(const AttnArgs& a, int64_t tokens, int bt) { return tiles_of(a.seqs, tokens, bt) + (a.fill ? 1 : 0); }
-double pairs_of(const AttnArgs& a) {  // of a dense request, as an upper bound for packed ones
-  const double nq = a.seqs.q_tokens, nk = a.seqs.k_tokens;
-  return double(a.seqs.batch) * a.q_heads * nq * nk * (a.causal ? 0.5 : 1.0);
+// Visible pairs of a dense request: of keys 1 .. nk that the last query sees, each
+// query before sees one less (causal), and none more than the window.  Where
+// lengths or offsets on the device cut it, no less than what they leave.
+double pairs_of(const AttnArgs& a) {
+  const double nq = a.seqs.q_tokens, nk = a.seqs.k_tokens, all = double(a.seqs.batch) * a.q_heads;
+  if (!a.causal) return all * nq * nk;
+  const double first = std::max(0.0, nk - nq), most = a.window ? std::min(double(a.window), nk) : nk;
+  const auto upto = [](double n) { return n * (n + 1) / 2; };
+  return all * (upto(most) - upto(std::min(first, most)) + most * (nk - std::max(first, most)));
 }
 
 // One tile of rows holds every query of every head of a group.

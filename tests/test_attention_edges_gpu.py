@@ -136,3 +136,21 @@ def test_rows_that_see_one_key_have_its_value_and_no_gradient(muon, case, dtype)
         lone = np.setdiff1d(first[at], [c for f, l in zip(first, last) if l > f for c in range(f, l + 1)])
         assert not row(dk, n)[torch.from_numpy(j + lone).cuda()].any(), n
     assert rows and dv.any()
+
+
+@pytest.mark.parametrize("case", [(2, 1, 1000, 4, 2, 64, True, 0), (1, 200, 200, 2, 2, 64, True, 50),
+                                  (1, 90, 40, 2, 1, 64, True, 0), (1, 90, 40, 2, 1, 64, True, 7),
+                                  (1, 30, 70, 2, 2, 64, True, 50), (1, 30, 70, 2, 2, 64, True, 10),
+                                  (3, 30, 70, 2, 2, 64, False, 0)], ids=str)
+def test_profile_counts_visible_pairs(muon, case):  # noqa: F811
+    b, sq, sk, hq, _, d, causal, window = case
+    q, k, v, do = make(case, "bf16")
+    kw = dict(causal=causal, window=window)
+    muon.profile(True)
+    out, lse = muon.attention(q, k, v, **kw)
+    muon.attention_backward(do, q, k, v, out, lse, **kw)
+    got = muon.profile_read()
+    muon.profile(False)
+    pairs = b * hq * int(ref.visible(sq, sk, causal, window).sum())
+    assert got["attention_forward"]["flops"] == 4 * pairs * d
+    assert got["attention_backward"]["flops"] == 10 * pairs * d
