@@ -336,7 +336,10 @@ typedef struct {
  * fill_rest).  Lengths and offsets beyond the axes are cut to them.
  *
  * Inputs that are not finite propagate; one that only some queries of a
- * sequence may see can also reach the others (0 * inf).
+ * sequence may see can also reach the others (0 * inf).  Infinities may come out
+ * as NaN: values (fp32) and probabilities (fp32, and bf16 in calls of few rows) are
+ * multiplied as two or three bf16 terms, which differ in sign and of which, from
+ * 2^128 (1 - 2^-9) on, the first is infinite.
  */
 typedef struct {
   int32_t dtype;           /* muon_dtype_t of q, k, v, out and gradients */

@@ -75,6 +75,21 @@ def test_rows_of_equal_probabilities_sum_to_one(muon, heads, d):  # noqa: F811
         assert not dv[i, n:].any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [(1, 70, 70, 2, 2, 64, True, 0), (1, 2, 1500, 4, 1, 128, False, 0)], ids=str)
+def test_infinite_values_reach_the_rows_that_see_them(muon, case, dtype):  # noqa: F811
+    """As infinity or NaN."""
+    import torch
+    q, k, v, _ = make(case, dtype)
+    at = case[2] // 2
+    v[0, at, :, 5] = INF
+    out, lse = muon.attention(q, k, v, causal=case[6])
+    seen = out[0, at if case[6] else 0:, :, 5]
+    assert not torch.isfinite(seen).any()
+    rest = torch.arange(case[5], device="cuda") != 5
+    assert torch.isfinite(out[..., rest]).all() and torch.isfinite(lse).all()
+
+
 def seen_keys(nq, nk, causal, window):
     """(first, last) key of each query."""
     i = np.arange(nq)
