@@ -335,6 +335,11 @@ typedef struct {
  * sequences; rows outside every sequence are left as they are (or see
  * fill_rest).  Lengths and offsets beyond the axes are cut to them.
  *
+ * Logits, statistics and sums are binary32.  bf16: p_j, and its gradient in the
+ * backward pass, is rounded to bf16 for the products it enters (2^-8 of each), or
+ * taken as two bf16 terms (2^-16) in calls of up to 4096 rows and for dq of heads
+ * of up to 32 elements.
+ *
  * Inputs that are not finite propagate; one that only some queries of a
  * sequence may see can also reach the others (0 * inf).  Infinities may come out
  * as NaN: values (fp32) and probabilities (fp32, and bf16 in calls of few rows) are
@@ -431,7 +436,9 @@ muon_status_t muon_validate_rotary(const muon_rotary_t* r, const muon_rotary_ten
  *   wk (its rows) *= sqrt(G)        wq (rows of h) *= g_h / sqrt(G)
  * so that head h's logits scale by g_h.  Rows whose factor is 1 are not
  * touched.  reset: then every max_logits entry becomes -inf, for the next
- * step's attention to raise. */
+ * step's attention to raise.  Weights that several devices hold a copy of need
+ * the largest logits over all of them before this call: each device's own would
+ * clip the copies apart. */
 typedef struct {
   void *wq, *wk;           /* in/out */
   float* max_logits;       /* device, [q_heads] */

@@ -63,7 +63,12 @@ class MuonAdamW(torch.optim.Optimizer):
         sets max_logits (fp32, [Hq]) to -inf for the next step's forward passes
         to raise (`attention(..., max_logits=...)`).  Views of packed weights
         are fine.  Nothing is read back to the host.  Not part of the state
-        dict: register after loading too."""
+        dict: register after loading too.
+
+        With copies of the weights on several ranks (data parallel), each rank's
+        max_logits are those of its own batch: reduce them before `step()`, or the
+        copies are clipped apart:
+            torch.distributed.all_reduce(max_logits, torch.distributed.ReduceOp.MAX)"""
         for t in (wq, wk, max_logits):
             if t.device.type != "cuda" or (t.device.index or 0) != self._device:
                 raise ValueError("clip_query_keys needs tensors on the parameters' GPU")

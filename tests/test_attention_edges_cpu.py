@@ -91,3 +91,39 @@ def test_scales_that_binary32_cannot_hold_in_base_2_are_refused():
     for g in (None, grads()):
         st, msg = check(request(scale=3e38), g)
         assert st == 1 and "scale" in msg
+
+
+# ---------------------------------------------------------------- copies of weights on several ranks
+
+def _clip_rank(rank, world, port, out):
+    import os
+    import numpy as np
+    import torch.distributed as dist
+    from oracle import attention_ref as ref
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port))
+    dist.init_process_group("gloo", rank=rank, world_size=world)
+    rng = np.random.default_rng(1)
+    wq, wk = rng.standard_normal((16, 4)), rng.standard_normal((8, 4))     # the same on every rank
+    top = torch.tensor([[8.0, 1.0], [2.0, 5.0]])[rank]                     # of the rank's batch
+    own = ref.qk_clip(wq, wk, top.numpy(), 4.0, "f32")
+    dist.all_reduce(top, dist.ReduceOp.MAX)
+    both = ref.qk_clip(wq, wk, top.numpy(), 4.0, "f32")
+    for name, res in (("own", own), ("both", both)):
+        mine = torch.from_numpy(np.concatenate([x[0].ravel() for x in res]))
+        all_ = [torch.empty_like(mine) for _ in range(world)]
+        dist.all_gather(all_, mine)
+        out[rank, name] = all(torch.equal(x, mine) for x in all_)
+    dist.destroy_process_group()
+
+
+def test_copies_of_weights_need_the_largest_logits_of_all_ranks():
+    """What `clip_query_keys` tells data-parallel programs to do, on the oracle."""
+    import socket
+    import torch.multiprocessing as mp
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    with mp.Manager() as m:
+        out = m.dict()
+        mp.spawn(_clip_rank, (2, port, out), nprocs=2)
+        assert all(out[r, "both"] for r in range(2)) and not any(out[r, "own"] for r in range(2))
