@@ -115,7 +115,7 @@ struct Lay {
 // PL = 3 bf16 planes, x = h + m + l (each the rounding of what the ones before
 // it leave; 8 bits each, so 24 in all unless l falls below bf16's range, from
 // |x| < 2^-109 on).  A product of two such values is hh + hm + mh + mm + hl +
-// lh, six bf16 MFMAs in fp32 accumulation; what is left out is 2^-24 of it.
+// lh, six bf16 MFMAs in fp32 accumulation; what is left out is 2^-23 of it at most.
 // (fp32 MFMAs have a sixteenth of the bf16 rate, so this is 2.7 times theirs.)
 template <int PL> struct Io { using T = uint16_t; };
 template <> struct Io<3> { using T = float; };
@@ -145,8 +145,8 @@ __device__ __forceinline__ void mma_acc(const Frag<PL>& a, const Frag<PA>& b, f3
   }
 }
 // Planes that probabilities and their gradients are taken in as operands: one
-// rounding to bf16 (2^-9 of each, as much as the result's own rounding costs),
-// three for fp32.  FINE: two, so that what is left is 2^-17; for requests of
+// rounding to bf16 (up to 2^-8 of each, as much as the result's own rounding costs),
+// three for fp32.  FINE: two, so that what is left is 2^-16; for requests of
 // few rows (fine_of), where single roundings do not average out and the
 // products cost little.
 template <int PL, bool FINE> constexpr int kAccPlanes = PL == 3 ? 3 : FINE ? 2 : 1;
@@ -1741,7 +1741,7 @@ bool eight_waves(const AttnArgs& a, int64_t workgroups, int64_t rows) {
 
 // Whether probabilities and their gradients are taken in two planes: where the
 // rows are few.  With one, an output's error is 1.4 times that of the exact one
-// rounded (2^-9 of each probability beside 2^-9 of the result), on average; of
+// rounded (up to 2^-8 of each probability beside 2^-8 of the result), on average; of
 // 300 random requests 7 with up to 4096 rows came to 1.5 to 2.  Query gradients
 // of heads of up to 32 elements too: the few keys that a query selects resemble
 // each other there, their terms cancel, and one plane leaves 1.6 times.

@@ -129,6 +129,7 @@ __device__ __forceinline__ uint2 tr_read_b64(const char* p) {
   return __builtin_bit_cast(uint2, v);
 }
 
+// Brackets one launch with the optional timer.
 struct Timed {
   LaunchTimer* t;
   int kind;

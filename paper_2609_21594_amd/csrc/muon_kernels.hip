@@ -1889,7 +1889,6 @@ hipError_t launch_gemm(int epi, GemmArgs ga, int nmat, hipStream_t st, double& e
   return hipGetLastError();
 }
 
-// Brackets one launch with the optional timer.
 // ---------------------------------------------------------------------------
 // Fused Newton-Schulz for the smaller matrices of short side up to 128
 // (k_ns_small; which, chunk_is_small): the whole step
