@@ -485,8 +485,9 @@ muon_status_t muon_plan_step(const muon_param_t* params, int64_t n, const muon_h
  * kernels), rotary, attention_forward, attention_backward, qk_clip (each call
  * one launch in the count; the flops of attention are 2 products' forward and
  * 5 products' backward over the visible pairs of the dense request: with lengths
- * or offsets, which lie on the device, an upper bound).  exec_flops of fp32 Newton-Schulz on the tile kernel counts its
- * six bf16 products.  `reset` != 0 clears the counters after reading. */
+ * or offsets, which lie on the device, an upper bound; calls captured into a
+ * graph are not counted).  exec_flops of fp32 Newton-Schulz on the tile kernel
+ * counts its six bf16 products.  `reset` != 0 clears the counters after reading. */
 typedef struct {
   const char* name;
   int64_t launches;

@@ -53,6 +53,17 @@ struct CurrentDevice {
   ~CurrentDevice() { if (prev >= 0) (void)hipSetDevice(prev); }
 };
 
+// The handle's timer, but not for launches that go into a graph: events recorded
+// there belong to its replays and cannot be waited for.
+muon::LaunchTimer* timer_on(muon_handle_t h, hipStream_t stream) {
+  muon::LaunchTimer* const t = muon::handle_timer(h);
+  if (!t) return nullptr;
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &capture) == hipSuccess) return capture == hipStreamCaptureStatusNone ? t : nullptr;
+  (void)hipGetLastError();
+  return nullptr;
+}
+
 int64_t elem_size(int dtype) { return dtype == MUON_BF16 ? 2 : 4; }
 bool known_dtype(int dtype) { return dtype == MUON_BF16 || dtype == MUON_F32; }
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
@@ -310,8 +321,8 @@ muon_status_t attend(muon_handle_t h, const muon_attention_t* a, const muon_atte
   if (!dev.ok) { muon::handle_error(h, "cannot select device %d", muon::handle_device(h)); return MUON_ERR_DEVICE; }
   const int dt = a->dtype == MUON_BF16 ? muon::DT_BF16 : muon::DT_F32;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = g ? muon::run_attention_backward(c.args, dt, s, muon::handle_timer(h))
-                         : muon::run_attention_forward(c.args, dt, s, muon::handle_timer(h));
+  const hipError_t e = g ? muon::run_attention_backward(c.args, dt, s, timer_on(h, s))
+                         : muon::run_attention_forward(c.args, dt, s, timer_on(h, s));
   if (e == hipSuccess) return MUON_OK;
   muon::handle_error(h, "kernel launch: %s", hipGetErrorString(e));
   return MUON_ERR_DEVICE;
@@ -419,7 +430,7 @@ muon_status_t rotary(muon_handle_t h, const muon_rotary_t* r, const muon_rotary_
   CurrentDevice dev(muon::handle_device(h));
   if (!dev.ok) { muon::handle_error(h, "cannot select device %d", muon::handle_device(h)); return MUON_ERR_DEVICE; }
   const hipError_t e = muon::run_rotary(k, r->dtype == MUON_BF16 ? muon::DT_BF16 : muon::DT_F32,
-                                        static_cast<hipStream_t>(stream), muon::handle_timer(h));
+                                        static_cast<hipStream_t>(stream), timer_on(h, static_cast<hipStream_t>(stream)));
   if (e == hipSuccess) return MUON_OK;
   muon::handle_error(h, "kernel launch: %s", hipGetErrorString(e));
   return MUON_ERR_DEVICE;
@@ -473,6 +484,7 @@ muon_status_t qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n,
   CurrentDevice dev(muon::handle_device(h));
   if (!dev.ok) { muon::handle_error(h, "cannot select device %d", muon::handle_device(h)); return MUON_ERR_DEVICE; }
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  muon::LaunchTimer* const timer = timer_on(h, s);
   int64_t all = 0;
   for (int64_t i = 0; i < n; ++i) all += (int64_t(entries[i].q_heads) + entries[i].kv_heads) * entries[i].head_dim;
   const int32_t per = all / muon::kClipRows >= 1024 ? muon::kClipRows : muon::kClipRowsFew;
@@ -506,8 +518,7 @@ muon_status_t qk_clip(muon_handle_t h, const muon_qk_clip_t* entries, int64_t n,
           ++k.n;
         }
         const hipError_t e = pass ? muon::run_reset_logits(k, s)
-                                  : muon::run_qk_clip(k, dt == MUON_BF16 ? muon::DT_BF16 : muon::DT_F32, s,
-                                                      muon::handle_timer(h));
+                                  : muon::run_qk_clip(k, dt == MUON_BF16 ? muon::DT_BF16 : muon::DT_F32, s, timer);
         if (e != hipSuccess) {
           muon::handle_error(h, "kernel launch: %s", hipGetErrorString(e));
           return MUON_ERR_DEVICE;

@@ -169,3 +169,39 @@ def test_profile_counts_visible_pairs(muon, case):  # noqa: F811
     pairs = b * hq * int(ref.visible(sq, sk, causal, window).sum())
     assert got["attention_forward"]["flops"] == 4 * pairs * d
     assert got["attention_backward"]["flops"] == 10 * pairs * d
+
+
+def test_profile_leaves_captured_calls_out(muon):  # noqa: F811
+    import torch
+    from paper_2609_21594_amd.attention import rotary_frequencies
+    q, k, v, do = make((1, 40, 40, 2, 2, 64, True, 0), "bf16")
+    freqs = rotary_frequencies(64).cuda()
+    w = [torch.ones(128, 8, device="cuda") for _ in range(2)]
+    top = torch.zeros(2, device="cuda")
+
+    def work():
+        a, b = muon.rotary([q, k], freqs)
+        out, lse = muon.attention(a, b, v, causal=True)
+        grads = muon.attention_backward(do, a, b, v, out, lse, causal=True)
+        muon.qk_clip([w[0]], [w[1]], [top], 1.0)
+        return [out, *grads]
+    eager = work()
+    torch.cuda.synchronize()
+    muon.profile(True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = work()
+    for _ in range(3):
+        for t in res:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(res, eager):
+            assert np.array_equal(to_bits(x), to_bits(y))
+    names = ("rotary", "attention_forward", "attention_backward", "qk_clip")
+    got = muon.profile_read()
+    assert all(got[n]["launches"] == 0 for n in names)
+    work()
+    got = muon.profile_read()
+    muon.profile(False)
+    assert all(got[n]["launches"] == 1 and got[n]["total_ms"] > 0 for n in names)
