@@ -308,7 +308,10 @@ muon_status_t muon_adamw_step(muon_handle_t h, const muon_adamw_param_t* params,
  *
  * A muon_heads_t is an array [batch][tokens][heads][head_dim] whose head_dim
  * elements are contiguous; strides in elements.  data and strides must be
- * multiples of 16 bytes (strides of dimensions of size 1 are ignored).
+ * multiples of 16 bytes (strides of dimensions of size 1 are ignored), tokens at
+ * most 2^24 bytes apart.  A call has at most 2^25 rows (query heads x tokens, of
+ * queries or keys) in 2^23 tiles (one for each 128 rows and one more for each head
+ * of each sequence), a rotation fewer than 2^24 tokens.
  * Strides of an input may be 0 (a broadcast input); an output's elements must
  * be distinct and must not meet any other buffer of the call.
  */

@@ -119,10 +119,11 @@ class _Rotary(torch.autograd.Function):
 
 
 def _plain(g):
-    """A gradient as the library takes it: contiguous, 16-byte aligned heads
-    (autograd also hands over expanded and sliced ones)."""
+    """A gradient as the library takes it: contiguous, 16-byte aligned heads, tokens
+    at most 2^24 bytes apart (autograd also hands over expanded and sliced ones)."""
     es = g.element_size()
-    if g.stride(-1) == 1 and g.data_ptr() % 16 == 0 and all(s * es % 16 == 0 and s > 0 for s in g.stride()[:-1]):
+    if (g.stride(-1) == 1 and g.data_ptr() % 16 == 0 and g.stride(-3) * es <= 1 << 24
+            and all(s * es % 16 == 0 and s > 0 for s in g.stride()[:-1])):
         return g
     return g.clone(memory_format=torch.contiguous_format)
 

@@ -127,3 +127,17 @@ def test_copies_of_weights_need_the_largest_logits_of_all_ranks():
         out = m.dict()
         mp.spawn(_clip_rank, (2, port, out), nprocs=2)
         assert all(out[r, "both"] for r in range(2)) and not any(out[r, "own"] for r in range(2))
+
+
+# ---------------------------------------------------------------- gradients as the library takes them
+
+def test_gradients_far_apart_are_copied():
+    """Tokens more than 2^24 bytes apart are refused by the library; autograd may hand
+    over such a gradient of an ordinary result."""
+    from paper_2609_21594_amd.attention import _plain
+    far = torch.zeros(2, (1 << 23) + 8, dtype=torch.bfloat16)
+    g = far[None, :, None, :64]
+    assert g.stride(1) * 2 > 1 << 24
+    assert _plain(g).is_contiguous()
+    near = torch.zeros(2, 1 << 12, dtype=torch.bfloat16).as_strided((1, 2, 2, 64), (4096, 128, 64, 1))
+    assert _plain(near) is near
