@@ -113,18 +113,25 @@ class _Rotary(torch.autograd.Function):
         need = [i for i, g in enumerate(gs) if g is not None and ctx.needs_input_grad[4 + i]]
         out = [None] * len(gs)
         if need:
-            for i, g in zip(need, ctx.lib.rotary([_plain(gs[i]) for i in need], freqs, positions=positions, **kw)):
+            for i, g in zip(need, ctx.lib.rotary([_near(gs[i]) for i in need], freqs, positions=positions, **kw)):
                 out[i] = g
         return (None, None, None, None, *out)
 
 
-def _plain(g):
-    """A gradient as the library takes it: contiguous, 16-byte aligned heads, tokens
-    at most 2^24 bytes apart (autograd also hands over expanded and sliced ones)."""
-    es = g.element_size()
-    if (g.stride(-1) == 1 and g.data_ptr() % 16 == 0 and g.stride(-3) * es <= 1 << 24
-            and all(s * es % 16 == 0 and s > 0 for s in g.stride()[:-1])):
+def _near(g):
+    """A gradient as the rotation takes it: contiguous heads, tokens at most 2^24
+    bytes apart (autograd also hands over transposed and sliced ones)."""
+    if g.stride(-1) == 1 and g.stride(-3) * g.element_size() <= 1 << 24:
         return g
+    return g.clone(memory_format=torch.contiguous_format)
+
+
+def _plain(g):
+    """A gradient as attention takes it: 16-byte aligned heads besides, none of them
+    expanded."""
+    es = g.element_size()
+    if g.data_ptr() % 16 == 0 and all(s * es % 16 == 0 and s > 0 for s in g.stride()[:-1]):
+        return _near(g)
     return g.clone(memory_format=torch.contiguous_format)
 
 

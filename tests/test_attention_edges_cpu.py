@@ -141,3 +141,31 @@ def test_gradients_far_apart_are_copied():
     assert _plain(g).is_contiguous()
     near = torch.zeros(2, 1 << 12, dtype=torch.bfloat16).as_strided((1, 2, 2, 64), (4096, 128, 64, 1))
     assert _plain(near) is near
+
+
+def test_rotary_copies_only_gradients_it_has_to():
+    """Its library call takes heads of any alignment, broadcast ones too, as long as
+    their elements are contiguous."""
+    class Rotary(StandIn):
+        def rotary(self, xs, freqs, positions=None, **kw):
+            self.got = xs
+            return super().rotary(xs, freqs, positions, **kw)
+    lib, seen = Rotary(), []
+    freqs = torch.ones(3, dtype=torch.float64)
+    from paper_2609_21594_amd import attention as A
+
+    class Ctx:
+        captured, kw, saved_tensors, needs_input_grad = False, dict(inverse=False), (freqs, None), (False,) * 4 + (True,)
+    Ctx.lib = lib
+    odd = torch.zeros(1, 5, 2, 7, dtype=torch.bfloat16)[..., 1:]             # 12-byte heads, 2-byte aligned
+    wide = torch.zeros(1, 1, 1, 6, dtype=torch.bfloat16).expand(1, 5, 2, 6)
+    turned = torch.zeros(1, 5, 6, 2, dtype=torch.bfloat16).transpose(2, 3)
+    capturing, A._enter_backward = A._enter_backward, lambda ctx: None       # (asks the device)
+    try:
+        for g in (odd, wide, turned):
+            A._Rotary.backward(Ctx, g)
+            seen.append(lib.got[0])
+    finally:
+        A._enter_backward = capturing
+    assert seen[0] is odd and seen[1] is wide
+    assert seen[2] is not turned and seen[2].is_contiguous()

@@ -5,7 +5,7 @@ import pytest
 
 from oracle import attention_ref as ref
 from tests.gpu_util import to_bits, to_host
-from tests.test_attention_gpu import close, make, muon  # noqa: F401
+from tests.test_attention_gpu import close, make, muon, tensor  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -205,3 +205,18 @@ def test_profile_leaves_captured_calls_out(muon):  # noqa: F811
     got = muon.profile_read()
     muon.profile(False)
     assert all(got[n]["launches"] == 1 and got[n]["total_ms"] > 0 for n in names)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_gradients_of_any_alignment(muon, dtype):  # noqa: F811
+    """Broadcast, sliced off their alignment and transposed ones, as autograd hands them over."""
+    import torch
+    from paper_2609_21594_amd.attention import rotary, rotary_frequencies
+    rng = np.random.default_rng(9)
+    freqs = rotary_frequencies(14).cuda()
+    x, wide, do = (tensor(rng, (2, 37, 3, n), dtype) for n in (20, 21, 20))
+    for g in (do, do[:, :1, :1].expand(2, 37, 3, 20), wide[..., 1:], do.transpose(2, 3).contiguous().transpose(2, 3)):
+        leaf = x.clone().requires_grad_()
+        rotary(muon, leaf, freqs, scale=1.5).backward(g)
+        close(leaf.grad, ref.rotary(to_host(g.contiguous()), np.broadcast_to(np.arange(37), (2, 37)), freqs.cpu().numpy(),
+                                    dtype, scale=1.5, inverse=True), "gradient")
