@@ -603,10 +603,10 @@ __device__ __forceinline__ KeyRange keys_of(const AttnArgs& a, const Seq& s, int
 // Bound by MFMA and vector issue together: per 64 keys and 32 queries of 128
 // elements 32 MFMAs (1024 cycles) and 32 x 4.2 vector instructions, of which 32
 // are exponentials (about 1000), overlapped across the waves of a SIMD in part
-// (MFMAs busy 55%, vector issue 53% of a busy CU's cycles, LDS 28%, no bank
-// conflicts).  4096 tokens, 32 heads on 8 of 128, causal: 136 us, 1015 TFLOP/s; 2
-// x 8192 without a mask: 1142; 4 x 4096, 16 heads of 64: 932; fp32, 2 x 2048, 16
-// heads of 128: 170.  Few rows: by memory, 268 MB of keys and values in 43 us.
+// (MFMAs busy 54%, vector issue 53% of a busy CU's cycles, LDS 27%, no bank
+// conflicts).  4096 tokens, 32 heads on 8 of 128, causal: 132 us, 1040 TFLOP/s; 2
+// x 8192 without a mask: 1170; 4 x 4096, 16 heads of 64: 970; fp32, 2 x 2048, 16
+// heads of 128: 162.  Few rows: by memory, 268 MB of keys and values in 45 us.
 // ---------------------------------------------------------------------------
 template <int PL, int DU, int BN, int WS, int NST, bool FINE, bool SPLIT, int NW>
 __global__ __launch_bounds__(64 * NW, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_fwd(AttnArgs a, int tiles, int pack) {
@@ -975,8 +975,9 @@ __device__ __forceinline__ float sum16(const f32x16_t& x) {
 // own sum tells the factor.  A sum further from 1 than such roundings is what lse
 // says (it may be that of more keys).  Rows so normalised also know what their
 // dS should sum to, which takes the rounding of out from delta.  Measured, errors
-// of dq and dk with logits of size 16 to 45: 0.4 to 1.1e-6 instead of 1.2 to
-// 2.7e-6, for 4% more time.
+// of dq and dk of 200 to 4000 tokens, heads of 64: 0.2 to 0.9e-6 instead of 0.3 to
+// 1.2e-6 with logits up to 24, heads of 128 up to 45: 1.9 to 2.2e-6 instead of 2.2
+// to 2.4e-6, for 5% more time.
 __device__ __forceinline__ float row_norm(float total, float lse2) {
   return total > 0.5f && fabsf(total - 1.f) <= 0x1p-22f * (fabsf(lse2) + 8.f) ? 1.f / total : 0.f;
 }
@@ -1009,7 +1010,7 @@ __device__ __forceinline__ float row_dots(const Frag<PL>* df, const char* out, c
 // from out where the caller kept it, and writes it and log2 of the sum of
 // exponentials for k_attn_dkv: +inf where no key is visible, so that every
 // probability recomputed from it is 0.  Bound as the forward pass is, with half
-// more products: 4096 tokens, 32 heads on 8 of 128, causal: 220 us (206 GFLOP,
+// more products: 4096 tokens, 32 heads on 8 of 128, causal: 223 us (206 GFLOP,
 // MFMAs busy 55%).
 template <int PL, int DU, int BN, int WS, int NST, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void k_attn_dq(AttnArgs a, int tiles) {
@@ -1185,7 +1186,7 @@ __global__ __launch_bounds__(256, WS == 1 && (PL == 1 || DU <= 64) ? 2 : 1) void
 // of the group: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  Its two
 // accumulators and K leave no registers for a second row of queries, so that a
 // step has 32 of them; V's place in LDS frees what two waves a SIMD need.  The
-// case above: 274 us (275 GFLOP, MFMAs busy 55%, LDS 41%).
+// case above: 279 us (275 GFLOP, MFMAs busy 55%, LDS 41%).
 template <int PL, int DU, int BM, int WS, int NST, bool VL, bool FINE>
 __global__ __launch_bounds__(256, WS == 1 && PL == 1 ? 2 : 1) void k_attn_dkv(AttnArgs a, int tiles) {
   constexpr int PA = kAccPlanes<PL, FINE>;
