@@ -341,7 +341,10 @@ typedef struct {
  * Logits, statistics and sums are binary32.  bf16: p_j, and its gradient in the
  * backward pass, is rounded to bf16 for the products it enters (2^-8 of each), or
  * taken as two bf16 terms (2^-16) in calls of up to 4096 rows and for dq of heads
- * of up to 32 elements.
+ * of up to 32 elements.  The backward pass recomputes p_j from lse, whose own
+ * rounding is then a common factor of a row's, up to exp(2^-23 |lse|): less than a
+ * step of bf16 for logits of 1e4, 1% for 1e6 (fp32: divided out, up to about 1e6).
+ * Logits of 1e8 and more have no useful gradients.
  *
  * Inputs that are not finite propagate; one that only some queries of a
  * sequence may see can also reach the others (0 * inf).  Infinities may come out

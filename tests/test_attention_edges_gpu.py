@@ -220,3 +220,33 @@ def test_rotary_gradients_of_any_alignment(muon, dtype):  # noqa: F811
         rotary(muon, leaf, freqs, scale=1.5).backward(g)
         close(leaf.grad, ref.rotary(to_host(g.contiguous()), np.broadcast_to(np.arange(37), (2, 37)), freqs.cpu().numpy(),
                                     dtype, scale=1.5, inverse=True), "gradient")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1e2, 1e3, 1e4])
+def test_one_key_far_above_the_others(muon, dtype, size):  # noqa: F811
+    """Logits of the size of diverged weights: out is that key's value, its dv the sum
+    of dout up to P's own rounding (two bf16 terms, 2^-16; fp32 2^-24), lse's (a
+    factor up to exp(2^-23 |lse|); fp32: divided out), the result's and that of a sum
+    of 20 rows."""
+    import torch
+    nq, n, d = 20, 70, 16
+    q, _, v, do = make((1, nq, n, 1, 1, d, False, 0), dtype)
+    k = torch.zeros_like(v)
+    q.zero_()
+    q[..., 0] = 1
+    k[0, :, 0, 0] = torch.linspace(-1, 0.5, n, device="cuda").to(k.dtype) * size
+    k[0, 35, 0, 0] = 1.0173 * size
+    res = torch.empty_like(q) if dtype == "bf16" else None
+    out, lse = muon.attention(q, k, v, scale=1.0, residual=res)
+    _, _, dv = muon.attention_backward(do, q, k, v, out, lse, residual=res, scale=1.0)
+    # scaled by log2 e and back: two constants, two products and a sum
+    top = float(k[0, 35, 0, 0])
+    assert (np.abs(to_host(lse) - top) <= 5 * 2.0 ** -24 * top).all()
+    u = ref.HALF_STEP[dtype]
+    # out: p of the key is 1 up to 2^-22 (exponential and sum), rounded
+    value = to_host(v)[0, 35, 0]
+    assert (np.abs(to_host(out)[0, :, 0] - value) <= (u + 2.0 ** -22) * np.abs(value)).all()
+    sums, sizes = to_host(do)[0, :, 0].sum(0), np.abs(to_host(do)[0, :, 0]).sum(0)
+    factor = np.expm1(2.0 ** -23 * float(lse.abs().max())) + 2.0 ** -16 if dtype == "bf16" else 14 * 2.0 ** -24
+    assert (np.abs(to_host(dv)[0, 35, 0] - sums) <= (factor + 24 * 2.0 ** -24) * sizes + u * np.abs(sums)).all()
