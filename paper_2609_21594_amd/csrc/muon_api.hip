@@ -1271,8 +1271,8 @@ bool buffers_disjoint(const Strided* b, size_t n) {
   if (!meet) return true;
   std::vector<Run> runs;
   for (size_t i = 0; i < n; ++i) {
-    // levels in order of their stride; a read-only one that repeats or
-    // overlaps itself is taken as its hull
+    // levels in order of their stride; a read-only one that overlaps itself is
+    // taken as its hull
     int order[3] = {0, 1, 2};
     const Strided& x = b[i];
     std::sort(order, order + 3, [&](int p, int q) { return x.stride[p] < x.stride[q]; });
@@ -1280,7 +1280,7 @@ bool buffers_disjoint(const Strided* b, size_t n) {
     bool nested = true;
     int m = 0;
     for (int k : order) {
-      if (x.count[k] == 1) continue;
+      if (x.count[k] == 1 || x.stride[k] == 0) continue;  // (a repeated one: the same bytes)
       nested = nested && x.stride[k] >= span;
       st[m] = x.stride[k];
       ct[m++] = x.count[k];

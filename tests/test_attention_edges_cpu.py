@@ -169,3 +169,23 @@ def test_rotary_copies_only_gradients_it_has_to():
         A._enter_backward = capturing
     assert seen[0] is odd and seen[1] is wide
     assert seen[2] is not turned and seen[2].is_contiguous()
+
+
+def test_broadcast_inputs_may_lie_between_outputs():
+    """Slices of one tensor, the keys' one head for all: no byte is shared."""
+    from tests.test_attention_cpu import BASE, check, grads, request
+    row = 20 * 64
+    fused = {f"{n}__{s}": x for n in ("q", "k", "v", "out") for s, x in (("token_stride", row), ("batch_stride", 96 * row))}
+    fused.update(q__data=BASE, k__data=BASE + 8 * 128, v__data=BASE + 9 * 128, out__data=BASE + 10 * 128,
+                 k__head_stride=0, v__head_stride=0)
+    assert check(request(**fused)) == (0, "")
+    # one sequence's keys for both
+    assert check(request(**dict(fused, k__batch_stride=0, v__batch_stride=0))) == (0, "")
+    # the keys' head is the last of the outputs'
+    assert "overlap" in check(request(**dict(fused, k__data=BASE + 17 * 128)))[1]
+    assert "overlap" in check(request(**dict(fused, k__data=BASE + 96 * row * 2 + 12 * 128, k__batch_stride=0)))[1]
+    g = grads()
+    for name, at in (("dq", 10), ("dk", 18)):
+        h = getattr(g, name)
+        h.data, h.token_stride, h.batch_stride = BASE + at * 128, row, 96 * row
+    assert check(request(**dict(fused, out__data=BASE + (40 << 32))), g) == (0, "")

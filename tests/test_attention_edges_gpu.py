@@ -250,3 +250,32 @@ def test_one_key_far_above_the_others(muon, dtype, size):  # noqa: F811
     sums, sizes = to_host(do)[0, :, 0].sum(0), np.abs(to_host(do)[0, :, 0]).sum(0)
     factor = np.expm1(2.0 ** -23 * float(lse.abs().max())) + 2.0 ** -16 if dtype == "bf16" else 14 * 2.0 ** -24
     assert (np.abs(to_host(dv)[0, 35, 0] - sums) <= (factor + 24 * 2.0 ** -24) * sizes + u * np.abs(sums)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_between_broadcast_inputs(muon, dtype):  # noqa: F811
+    """All in one tensor, one head of keys and values for all query heads."""
+    import torch
+    q, k, v, do = make((2, 70, 70, 4, 1, 64, True, 0), dtype)
+    want = ref.attention(*map(to_host, (q, k, v)), dtype, causal=True, dout=to_host(do))
+    buf = torch.full((2, 70, 22, 64), 5.0, dtype=q.dtype, device="cuda")
+    q2, k2, v2, do2, out, dq = (buf[:, :, a:b] for a, b in ((0, 4), (4, 5), (5, 6), (6, 10), (10, 14), (14, 18)))
+    for t, s in ((q2, q), (k2, k), (v2, v), (do2, do)):
+        t.copy_(s)
+    kx, vx = k2.expand(2, 70, 4, 64), v2.expand(2, 70, 4, 64)
+    res = torch.empty_like(q) if dtype == "bf16" else None
+    _, lse = muon.attention(q2, kx, vx, causal=True, out=out, residual=res)
+    close(out.contiguous(), want["out"], "out")
+    exact = torch.from_numpy(want["out"][0]).cuda()
+    out.copy_(exact)
+    res = (exact - out.double()).to(torch.bfloat16) if res is not None else None
+    lse = torch.from_numpy(want["lse"][0]).float().cuda()
+    _, dk, dv = muon.attention_backward(do2, q2, kx, vx, out, lse, residual=res, causal=True, dq=dq)
+    close(dq.contiguous(), want["dq"], "dq")
+    # a gradient for each head that sees the one: together its own
+    for name, x in (("dk", dk), ("dv", dv)):
+        val, bound = want[name]
+        each = to_host(x)
+        slack = ref.HALF_STEP[dtype] * np.abs(each).sum(2, keepdims=True)
+        assert (np.abs(each.sum(2, keepdims=True) - val) <= bound + slack * (1 + 2.0 ** -7)).all(), name
+    assert (buf[:, :, 18:] == 5).all() and torch.equal(q2, q) and torch.equal(do2, do)
