@@ -344,7 +344,7 @@ typedef struct {
  * of up to 32 elements.  The backward pass recomputes p_j from lse, whose own
  * rounding is then a common factor of a row's, up to exp(2^-23 |lse|): less than a
  * step of bf16 for logits of 1e4, 1% for 1e6 (fp32: divided out, up to about 1e6).
- * Logits of 1e8 and more have no useful gradients.
+ * Logits of 1e8 and more have no useful gradients, from 2^31 on no useful results.
  *
  * Inputs that are not finite propagate; one that only some queries of a
  * sequence may see can also reach the others (0 * inf).  Infinities may come out
